@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libxkv.so")
-SOURCES = ["xkv_host.cu", "xkv_maint.cu", "xkv_attn_simple.cu", "xkv_attn_tc.cu"]
+SOURCES = ["xkv_host.cu", "xkv_maint.cu", "xkv_attn_simple.cu", "xkv_attn_tc.cu",
+           "xkv_paged_host.cu", "xkv_paged_tokens.cu", "xkv_paged_simple.cu", "xkv_paged_evict.cu"]
 
 
 def _nvcc() -> str:
@@ -21,7 +22,8 @@ def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "xkv.h")]
+    include = os.path.join(ROOT, "include")
+    deps = [os.path.join(d, f) for d in (CSRC, include) for f in os.listdir(d)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -1,0 +1,281 @@
+// Host side of the paged cache and of the rotary positions: argument checks, the handle, the C ABI.
+#include <math.h>
+#include <string.h>
+
+#include <mutex>
+#include <new>
+
+#include "xkv_paged_internal.cuh"
+
+using namespace xkv;
+
+namespace {
+
+constexpr int kMaxDevices = 64;
+constexpr int kMaxHeads = 64;
+constexpr int64_t kMaxStride = (int64_t)1 << 38;       // elements; a tensor map's strides stay below 2^40 bytes
+
+// Per device, on first use with that device current: the number of multiprocessors and the kernels' attributes.
+std::mutex g_setup_mutex;
+int g_sm_count[kMaxDevices] = {0};
+
+int device_setup(int* device, int* sm_count) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return XKV_E_CUDA;
+  if (dev < 0 || dev >= kMaxDevices) return XKV_E_UNSUPPORTED;
+  std::lock_guard<std::mutex> lock(g_setup_mutex);
+  if (g_sm_count[dev] == 0) {
+    int sms = 0;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return XKV_E_CUDA;
+    if (evict_device_setup() != cudaSuccess) return XKV_E_CUDA;
+    g_sm_count[dev] = sms;
+  }
+  *device = dev;
+  *sm_count = g_sm_count[dev];
+  return XKV_OK;
+}
+
+bool aligned(const void* p, size_t a) { return p && (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < kMaxStride; }
+// A token tensor of `heads` heads.
+bool tensor_ok(const void* p, int64_t ts, int64_t hs) { return aligned(p, 16) && stride_ok(ts) && stride_ok(hs); }
+
+int log2_of(int x) {
+  int l = 0;
+  while ((1 << l) < x) ++l;
+  return l;
+}
+
+bool params_ok(const xkv_paged_params* p) {
+  if (!p || p->reserved != 0) return false;
+  if (p->n_kv_heads < 1 || p->n_kv_heads > kMaxHeads || p->n_heads < 1 || p->n_heads > kMaxHeads || p->n_heads % p->n_kv_heads) return false;
+  if (p->head_dim != 64 && p->head_dim != 128) return false;
+  if (p->dtype != XKV_BF16 && p->dtype != XKV_FP16) return false;
+  if (p->page_tokens < 16 || p->page_tokens > 256 || (p->page_tokens & (p->page_tokens - 1))) return false;
+  if (p->n_pages < 1 || p->max_seqs < 1 || p->max_seqs > kMaxSeqs) return false;
+  if (!stride_ok(p->page_stride) || !stride_ok(p->head_stride) || !stride_ok(p->slot_stride)) return false;
+  return p->slot_stride >= p->head_dim;
+}
+
+// Workspace: the status word.
+size_t workspace_bytes(const xkv_paged_params*, int) { return 256; }
+
+bool batch_ok(const xkv_paged* c, const xkv_paged_batch* b, bool tokens) {
+  if (!b || b->n_seqs < 1 || b->n_seqs > c->p.max_seqs || b->table_width < 0) return false;
+  if ((int64_t)b->table_width * c->p.page_tokens >= ((int64_t)1 << 31) - (1 << 16)) return false;
+  if (!aligned(b->lens, 4) || (b->table_width > 0 && !aligned(b->table, 4))) return false;
+  if (!tokens) return true;
+  return b->n_tokens >= 0 && b->n_tokens <= (1 << 28) && b->max_new >= 0 && aligned(b->q_start, 4);
+}
+
+SeqView seq_view(const xkv_paged_batch* b) {
+  SeqView s;
+  s.n_seqs = b->n_seqs; s.n_tokens = b->n_tokens; s.max_new = b->max_new; s.table_width = b->table_width;
+  s.q_start = b->q_start; s.lens = b->lens; s.table = b->table;
+  return s;
+}
+
+// Turns per position of every pair of an axis.
+bool plan_rotary(const xkv_rotary_params* p, int head_dim, bool inverse, const int32_t* positions, int64_t pos_stride, int n, RotaryPlan* r) {
+  if (!p || p->n_axes < 1 || p->n_axes > 4 || p->rotary_dim < 2 || p->rotary_dim % 2 || p->rotary_dim > head_dim ||
+      p->rotary_dim * p->n_axes > head_dim) return false;
+  if (!(p->base > 1.0) || !(p->factor >= 1.0) || !(p->magnitude > 0.0) || !isfinite(p->base) || !isfinite(p->factor) || !isfinite(p->magnitude)) return false;
+  if (p->original_tokens < 0) return false;
+  if (p->original_tokens > 0 && (!(p->beta_slow >= 0.0) || !(p->beta_fast > p->beta_slow) || !isfinite(p->beta_fast))) return false;
+  if (n > 0 && !aligned(positions, 4)) return false;
+  if (p->n_axes > 1 && pos_stride < n) return false;
+  r->axes = p->n_axes; r->rot = p->rotary_dim; r->pairs = p->rotary_dim / 2; r->interleaved = p->interleaved != 0;
+  r->magnitude = (float)p->magnitude;
+  r->positions = positions; r->pos_stride = pos_stride;
+  const double two_pi = 6.283185307179586476925286766559;
+  for (int i = 0; i < r->pairs; ++i) {
+    double w = pow(p->base, -2.0 * i / p->rotary_dim);
+    if (p->original_tokens > 0) {
+      double keep = (p->original_tokens * w / two_pi - p->beta_slow) / (p->beta_fast - p->beta_slow);
+      keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+      w = w * keep + w / p->factor * (1.0 - keep);
+    } else {
+      w /= p->factor;
+    }
+    r->turns[i] = (inverse ? -w : w) / two_pi;
+  }
+  return true;
+}
+
+TokenTensor token_tensor(const void* in, int64_t its, int64_t ihs, void* out, int64_t ots, int64_t ohs, int heads) {
+  TokenTensor t;
+  t.in = reinterpret_cast<const uint8_t*>(in); t.out = reinterpret_cast<uint8_t*>(out);
+  t.in_ts = its; t.in_hs = ihs; t.out_ts = ots; t.out_hs = ohs; t.heads = heads;
+  return t;
+}
+
+// The handle's device has to be the current one.
+int on_device(const xkv_paged* c) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return XKV_E_CUDA;
+  return dev == c->device ? XKV_OK : XKV_E_INVALID;
+}
+
+int from_cuda(cudaError_t e) {
+  return e == cudaSuccess ? XKV_OK : e == cudaErrorNotSupported ? XKV_E_UNSUPPORTED : XKV_E_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+int xkv_rotary(const xkv_rotary_params* params, int32_t dtype, int32_t head_dim, const int32_t* positions, int64_t pos_stride, int32_t n,
+               const void* q, void* q_out, int32_t n_q_heads, int64_t q_ts, int64_t q_hs, int64_t qo_ts, int64_t qo_hs,
+               const void* k, void* k_out, int32_t n_k_heads, int64_t k_ts, int64_t k_hs, int64_t ko_ts, int64_t ko_hs,
+               int32_t inverse, xkv_stream stream) {
+  if (dtype != XKV_BF16 && dtype != XKV_FP16) return XKV_E_INVALID;
+  if (head_dim < 8 || head_dim > 2 * kMaxPairs || head_dim % 8) return XKV_E_INVALID;
+  if (n < 0 || n > (1 << 28) || n_q_heads < 1 || n_q_heads > 1024 || n_k_heads < 0 || n_k_heads > 1024) return XKV_E_INVALID;
+  TokenArgs a;
+  memset(&a, 0, sizeof(a));
+  if (!plan_rotary(params, head_dim, inverse != 0, positions, pos_stride, n, &a.rot)) return XKV_E_INVALID;
+  if (n == 0) return XKV_OK;
+  if (!tensor_ok(q, q_ts, q_hs) || !tensor_ok(q_out, qo_ts, qo_hs)) return XKV_E_INVALID;
+  if (n_k_heads > 0 && (!tensor_ok(k, k_ts, k_hs) || !tensor_ok(k_out, ko_ts, ko_hs))) return XKV_E_INVALID;
+  if ((q == q_out && (q_ts != qo_ts || q_hs != qo_hs)) || (n_k_heads > 0 && k == k_out && (k_ts != ko_ts || k_hs != ko_hs))) return XKV_E_INVALID;
+  int dev, sms;
+  const int rc = device_setup(&dev, &sms);
+  if (rc != XKV_OK) return rc;
+  a.n = n; a.head_dim = head_dim;
+  a.q = token_tensor(q, q_ts, q_hs, q_out, qo_ts, qo_hs, n_q_heads);
+  a.k = token_tensor(k, k_ts, k_hs, k_out, ko_ts, ko_hs, n_k_heads);
+  return from_cuda(launch_tokens(a, dtype, sms, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t xkv_paged_workspace_bytes(const xkv_paged_params* params, int32_t multiprocessors) {
+  if (!params_ok(params) || multiprocessors < 1 || multiprocessors > 1024) return 0;
+  return workspace_bytes(params, multiprocessors);
+}
+
+int xkv_paged_create(const xkv_paged_params* params, void* k_pages, void* v_pages, float* weights, void* dev_workspace, size_t bytes,
+                     xkv_stream stream, xkv_paged** out) {
+  if (!out) return XKV_E_INVALID;
+  *out = nullptr;
+  if (!params) return XKV_E_INVALID;
+  if (!params_ok(params)) {
+    if (params->head_dim > 0 && params->head_dim != 64 && params->head_dim != 128) return XKV_E_UNSUPPORTED;
+    if (params->page_tokens > 0 && (params->page_tokens < 16 || params->page_tokens > 256 || (params->page_tokens & (params->page_tokens - 1))))
+      return XKV_E_UNSUPPORTED;
+    return XKV_E_INVALID;
+  }
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || (weights && !aligned(weights, 4)) || !aligned(dev_workspace, 256)) return XKV_E_INVALID;
+  int dev, sms;
+  const int rc = device_setup(&dev, &sms);
+  if (rc != XKV_OK) return rc;
+  const size_t need = workspace_bytes(params, sms);
+  if (bytes < need) return XKV_E_NOMEM;
+  xkv_paged* c = new (std::nothrow) xkv_paged;
+  if (!c) return XKV_E_NOMEM;
+  memset(c, 0, sizeof(*c));
+  c->p = *params;
+  c->device = dev;
+  c->sm_count = sms;
+  c->ws = reinterpret_cast<uint8_t*>(dev_workspace);
+  c->ws_bytes = need;
+  PagedView& v = c->view;
+  v.k = reinterpret_cast<uint8_t*>(k_pages); v.v = reinterpret_cast<uint8_t*>(v_pages); v.weights = weights;
+  v.page_stride = params->page_stride; v.head_stride = params->head_stride; v.slot_stride = params->slot_stride;
+  v.n_heads = params->n_heads; v.n_kv_heads = params->n_kv_heads; v.group = params->n_heads / params->n_kv_heads;
+  v.page_shift = log2_of(params->page_tokens); v.n_pages = params->n_pages;
+  v.status = reinterpret_cast<int*>(c->ws);
+  if (cudaMemsetAsync(c->ws, 0, need, reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess) { delete c; return XKV_E_CUDA; }
+  *out = c;
+  return XKV_OK;
+}
+
+int xkv_paged_destroy(xkv_paged* c) {
+  if (!c) return XKV_E_INVALID;
+  delete c;
+  return XKV_OK;
+}
+
+int xkv_paged_poll_status(xkv_paged* c, xkv_stream stream) {
+  if (!c) return XKV_E_INVALID;
+  const int rc = on_device(c);
+  if (rc != XKV_OK) return rc;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  int v = 0;
+  if (cudaMemcpyAsync(&v, c->view.status, sizeof(v), cudaMemcpyDeviceToHost, st) != cudaSuccess) return XKV_E_CUDA;
+  if (cudaStreamSynchronize(st) != cudaSuccess) return XKV_E_CUDA;
+  if (v != 0 && cudaMemsetAsync(c->view.status, 0, sizeof(v), st) != cudaSuccess) return XKV_E_CUDA;
+  return v;
+}
+
+int kv_paged_append(xkv_paged* c, const xkv_paged_batch* b, const void* k, int64_t k_ts, int64_t k_hs, const void* v, int64_t v_ts, int64_t v_hs,
+                    const void* q, int64_t q_ts, int64_t q_hs, void* q_out, int64_t qo_ts, int64_t qo_hs,
+                    const xkv_rotary_params* rotary, const int32_t* positions, int64_t pos_stride, xkv_stream stream) {
+  if (!c || !batch_ok(c, b, true)) return XKV_E_INVALID;
+  TokenArgs a;
+  memset(&a, 0, sizeof(a));
+  if (rotary && !plan_rotary(rotary, c->p.head_dim, false, positions, pos_stride, b->n_tokens, &a.rot)) return XKV_E_INVALID;
+  const int rc = on_device(c);
+  if (rc != XKV_OK) return rc;
+  if (b->n_tokens == 0) return XKV_OK;
+  if (!tensor_ok(k, k_ts, k_hs) || !tensor_ok(v, v_ts, v_hs)) return XKV_E_INVALID;
+  if (q && (!tensor_ok(q, q_ts, q_hs) || !tensor_ok(q_out, qo_ts, qo_hs) || (q == q_out && (q_ts != qo_ts || q_hs != qo_hs)))) return XKV_E_INVALID;
+  a.n = b->n_tokens; a.head_dim = c->p.head_dim; a.append = 1;
+  if (q) a.q = token_tensor(q, q_ts, q_hs, q_out, qo_ts, qo_hs, c->p.n_heads);
+  a.k = token_tensor(k, k_ts, k_hs, nullptr, 0, 0, c->p.n_kv_heads);
+  a.v = token_tensor(v, v_ts, v_hs, nullptr, 0, 0, c->p.n_kv_heads);
+  a.cache = c->view; a.seqs = seq_view(b);
+  return from_cuda(launch_tokens(a, c->p.dtype, c->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+int attn_paged_causal(xkv_paged* c, const xkv_paged_batch* b, const void* q, int64_t q_ts, int64_t q_hs, void* out, int64_t o_ts, int64_t o_hs,
+                      float* lse, float scale, int32_t mask, int32_t impl, xkv_stream stream) {
+  if (!c || !batch_ok(c, b, true) || !(scale > 0.f) || !isfinite(scale) || (mask != XKV_MASK_CAUSAL && mask != XKV_MASK_FULL) || (impl != 0 && impl != 1))
+    return XKV_E_INVALID;
+  const int rc = on_device(c);
+  if (rc != XKV_OK) return rc;
+  if (b->n_tokens == 0 || b->max_new == 0) return XKV_OK;
+  if (!tensor_ok(q, q_ts, q_hs) || !tensor_ok(out, o_ts, o_hs) || (lse && !aligned(lse, 4))) return XKV_E_INVALID;
+  PagedAttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.cache = c->view; a.seqs = seq_view(b);
+  a.q = reinterpret_cast<const uint8_t*>(q); a.q_ts = q_ts; a.q_hs = q_hs;
+  a.out = reinterpret_cast<uint8_t*>(out); a.o_ts = o_ts; a.o_hs = o_hs;
+  a.lse = lse; a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f; a.full = mask == XKV_MASK_FULL;
+  return from_cuda(launch_paged_attn_simple(a, c->p.head_dim, c->p.dtype, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+int kv_paged_weights(xkv_paged* c, const xkv_paged_batch* b, const void* q, int64_t q_ts, int64_t q_hs, const float* lse, float scale, float decay,
+                     int32_t mask, xkv_stream stream) {
+  if (!c || !batch_ok(c, b, true) || !(scale > 0.f) || !isfinite(scale) || !(decay >= 0.f) || !isfinite(decay) ||
+      (mask != XKV_MASK_CAUSAL && mask != XKV_MASK_FULL)) return XKV_E_INVALID;
+  const int rc = on_device(c);
+  if (rc != XKV_OK) return rc;
+  if (!c->view.weights) return XKV_E_STATE;
+  if (b->n_tokens == 0 || b->max_new == 0 || b->table_width == 0) return XKV_OK;
+  if (!tensor_ok(q, q_ts, q_hs) || !aligned(lse, 4)) return XKV_E_INVALID;
+  PagedWeightArgs a;
+  memset(&a, 0, sizeof(a));
+  a.cache = c->view; a.seqs = seq_view(b);
+  a.q = reinterpret_cast<const uint8_t*>(q); a.q_ts = q_ts; a.q_hs = q_hs;
+  a.lse = lse; a.scale_log2 = scale * 1.4426950408889634f; a.decay = decay; a.full = mask == XKV_MASK_FULL;
+  return from_cuda(launch_paged_weights_simple(a, c->p.head_dim, c->p.dtype, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+int kv_paged_evict(xkv_paged* c, const xkv_paged_batch* b, const int32_t* dst_table, int32_t dst_width, int32_t keep, int32_t n_first,
+                   int32_t n_recent, int32_t* kept, int32_t* lens_out, xkv_stream stream) {
+  if (!c || !batch_ok(c, b, false)) return XKV_E_INVALID;
+  if (keep < 1 || n_first < 0 || n_recent < 0 || (int64_t)n_first + n_recent > keep) return XKV_E_INVALID;
+  if (dst_width < 1 || (int64_t)dst_width * c->p.page_tokens < keep || (int64_t)dst_width * c->p.page_tokens >= ((int64_t)1 << 31) - (1 << 16))
+    return XKV_E_INVALID;
+  if (!aligned(dst_table, 4) || !aligned(kept, 4) || !aligned(lens_out, 4)) return XKV_E_INVALID;
+  const int rc = on_device(c);
+  if (rc != XKV_OK) return rc;
+  if (!c->view.weights) return XKV_E_STATE;
+  EvictArgs a;
+  memset(&a, 0, sizeof(a));
+  a.cache = c->view; a.seqs = seq_view(b);
+  a.dst_table = dst_table; a.dst_width = dst_width; a.keep = keep; a.n_first = n_first; a.n_recent = n_recent;
+  a.head_dim = c->p.head_dim; a.kept = kept; a.lens_out = lens_out;
+  return from_cuda(launch_evict(a, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"

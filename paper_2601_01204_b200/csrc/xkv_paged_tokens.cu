@@ -1,0 +1,226 @@
+// Rotary positions and the append to the pages: one kernel that reads every token row once and writes it once.
+//
+// A block takes a few tokens.  Their sines and cosines are computed once, in shared memory, and serve all heads:
+// the angle is formed as position * (turns per position) in 64 bits, its whole turns are dropped there, and what is
+// left (at most half a turn) goes to sincospif in 32 bits.  64 positions of a full head cost 4 096 such angles, the rows
+// that they turn (40 heads of 128 channels) 1.3 MB of traffic.  After that a thread moves 16 or 32 bytes of a row
+// at a time: a pair of 16-byte pieces half an axis apart, or one piece of interleaved pairs.
+#include "xkv_paged_internal.cuh"
+
+namespace xkv {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTok = 16;              // tokens of a block
+
+template <typename T> struct Two;
+template <> struct Two<__nv_bfloat16> {
+  static __device__ __forceinline__ float2 get(uint32_t u) {
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint32_t put(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float one(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
+};
+template <> struct Two<__half> {
+  static __device__ __forceinline__ float2 get(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
+  static __device__ __forceinline__ uint32_t put(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float one(uint16_t u) { return __half2float(*reinterpret_cast<const __half*>(&u)); }
+};
+
+// VEC: every axis is whole 16-byte pieces (rotary_dim a multiple of 16, of 8 when interleaved); otherwise a thread
+// turns one pair or copies one channel at a time.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant__ TokenArgs a, int tok_per_block, int items_log2) {
+  __shared__ float2 s_cs[kMaxTok][kMaxPairs];
+  __shared__ int64_t s_page[kMaxTok];         // row offset of the token's slot at head 0, -1: not written
+  __shared__ int64_t s_weight[kMaxTok];
+  grid_dependency_wait();
+  const int tok0 = blockIdx.x * tok_per_block;
+  const int toks = min(tok_per_block, a.n - tok0);
+  const int all_pairs = a.rot.axes * a.rot.pairs;
+  const int tid = threadIdx.x;
+  for (int e = tid; e < toks * all_pairs; e += kThreads) {
+    const int t = e / all_pairs, p = e - t * all_pairs;
+    const int axis = p / a.rot.pairs, i = p - axis * a.rot.pairs;
+    const double x = (double)a.rot.positions[axis * a.rot.pos_stride + tok0 + t] * a.rot.turns[i];
+    const double part = x - rint(x);                   // in [-1/2, 1/2] turns
+    float s, c;
+    sincospif(2.f * (float)part, &s, &c);
+    s_cs[t][p] = make_float2(c * a.rot.magnitude, s * a.rot.magnitude);
+  }
+  if (a.append && tid < toks) {
+    const int row = tok0 + tid;
+    // the sequence whose rows hold this one: the last with q_start <= row
+    int lo = 0, hi = a.seqs.n_seqs;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.seqs.q_start[mid] <= row) lo = mid; else hi = mid;
+    }
+    const Seq q = seq_at(a.cache, a.seqs, lo);
+    s_page[tid] = -1;
+    s_weight[tid] = -2;                                  // nobody's row
+    if (row >= q.row0 && row < q.row0 + q.n_new) {
+      s_weight[tid] = -1;
+      const int slot = q.len - q.n_new + (row - q.row0);
+      const int page = slot >= 0 ? page_at(a.cache, a.seqs.table, a.seqs.table_width, lo, slot) : -1;
+      if (page >= 0) {
+        s_page[tid] = row_offset(a.cache, page, 0, slot);
+        s_weight[tid] = weight_offset(a.cache, page, 0, slot);
+      }
+    }
+  }
+  __syncthreads();
+  const int lanes = 1 << items_log2;                     // threads that share a row
+  const int item = tid & (lanes - 1);
+  const int heads = a.q.heads + a.k.heads + a.v.heads;
+  const int half = a.rot.rot >> 1;
+  const int turned = a.rot.axes * a.rot.rot;             // channels
+  // what this thread does in a row: a pair of places to turn, or a place to copy
+  constexpr int kW = VEC ? 8 : 1;                        // channels of a place
+  int c0 = 0, c1 = -1, pair = -1;
+  bool active;
+  if (VEC && a.rot.interleaved) {
+    active = item < a.head_dim / 8;
+    c0 = item * 8;
+    if (c0 < turned) pair = c0 >> 1;
+  } else {
+    // items [0, turned / 2 / kW): (axis, place in its first half); then the places behind
+    const int pairs = turned / 2 / kW;
+    active = item < pairs + (a.head_dim - turned) / kW;
+    if (item < pairs) {
+      if (a.rot.interleaved) { pair = item; c0 = 2 * item; c1 = c0 + 1; }
+      else {
+        const int per = half / kW;
+        const int axis = item / per, i = item - axis * per;
+        c0 = axis * a.rot.rot + i * kW;
+        c1 = c0 + half;
+        pair = axis * a.rot.pairs + i * kW;
+      }
+    } else {
+      c0 = turned + (item - pairs) * kW;
+    }
+  }
+  if (!active) return;
+  const int step = kThreads >> items_log2;
+  constexpr int kU = 4;                                  // rows in flight per thread
+  // blockIdx.y: a share of the heads
+  const int h_per = (heads + gridDim.y - 1) / gridDim.y, h_lo = blockIdx.y * h_per;
+  const int h_n = min(h_per, heads - h_lo);
+  const int total = toks * max(h_n, 0);
+  for (int base = tid >> items_log2; base < total; base += kU * step) {
+    uint4 x0[kU], x1[kU];
+    uint8_t* dst[kU];
+    int tk[kU];
+    bool rotate[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int c = base + u * step;
+      dst[u] = nullptr;
+      if (c >= total) continue;
+      const int t = c / h_n;
+      int h = h_lo + (c - t * h_n);
+      const int row = tok0 + t;
+      tk[u] = t;
+      rotate[u] = true;
+      if (a.append && s_weight[t] == -2) continue;       // nobody's row
+      const uint8_t* src;
+      if (h < a.q.heads) {
+        src = a.q.in + 2 * ((int64_t)h * a.q.in_hs + (int64_t)row * a.q.in_ts);
+        dst[u] = a.q.out + 2 * ((int64_t)h * a.q.out_hs + (int64_t)row * a.q.out_ts);
+      } else if ((h -= a.q.heads) < a.k.heads) {
+        src = a.k.in + 2 * ((int64_t)h * a.k.in_hs + (int64_t)row * a.k.in_ts);
+        if (a.append) {
+          if (s_page[t] < 0) continue;
+          dst[u] = a.cache.k + 2 * (s_page[t] + (int64_t)h * a.cache.head_stride);
+          if (item == 0 && a.cache.weights)
+            a.cache.weights[s_weight[t] + ((int64_t)h << a.cache.page_shift)] = 0.f;
+        } else {
+          dst[u] = a.k.out + 2 * ((int64_t)h * a.k.out_hs + (int64_t)row * a.k.out_ts);
+        }
+      } else {
+        h -= a.k.heads;
+        if (s_page[t] < 0) continue;
+        src = a.v.in + 2 * ((int64_t)h * a.v.in_hs + (int64_t)row * a.v.in_ts);
+        dst[u] = a.cache.v + 2 * (s_page[t] + (int64_t)h * a.cache.head_stride);
+        rotate[u] = false;
+      }
+      if (VEC) {
+        x0[u] = *reinterpret_cast<const uint4*>(src + 2 * c0);
+        if (c1 >= 0) x1[u] = *reinterpret_cast<const uint4*>(src + 2 * c1);
+      } else {
+        x0[u].x = *reinterpret_cast<const uint16_t*>(src + 2 * c0);
+        if (c1 >= 0) x1[u].x = *reinterpret_cast<const uint16_t*>(src + 2 * c1);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      if (!dst[u]) continue;
+      if (pair >= 0 && rotate[u]) {
+        const float2* cs = &s_cs[tk[u]][pair];
+        if (VEC && c1 < 0) {                             // interleaved: four pairs of one piece
+          uint32_t* w = &x0[u].x;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 x = Two<T>::get(w[i]), r = cs[i];
+            w[i] = Two<T>::put(x.x * r.x - x.y * r.y, x.y * r.x + x.x * r.y);
+          }
+        } else if (VEC) {
+          uint32_t* w0 = &x0[u].x;
+          uint32_t* w1 = &x1[u].x;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 x = Two<T>::get(w0[i]), y = Two<T>::get(w1[i]), r = cs[2 * i], s = cs[2 * i + 1];
+            w0[i] = Two<T>::put(x.x * r.x - y.x * r.y, x.y * s.x - y.y * s.y);
+            w1[i] = Two<T>::put(y.x * r.x + x.x * r.y, y.y * s.x + x.y * s.y);
+          }
+        } else {
+          const float x = Two<T>::one((uint16_t)x0[u].x), y = Two<T>::one((uint16_t)x1[u].x);
+          x0[u].x = Two<T>::put(x * cs->x - y * cs->y, 0.f) & 0xFFFFu;
+          x1[u].x = Two<T>::put(y * cs->x + x * cs->y, 0.f) & 0xFFFFu;
+        }
+      }
+      if (VEC) {
+        *reinterpret_cast<uint4*>(dst[u] + 2 * c0) = x0[u];
+        if (c1 >= 0) *reinterpret_cast<uint4*>(dst[u] + 2 * c1) = x1[u];
+      } else {
+        *reinterpret_cast<uint16_t*>(dst[u] + 2 * c0) = (uint16_t)x0[u].x;
+        if (c1 >= 0) *reinterpret_cast<uint16_t*>(dst[u] + 2 * c1) = (uint16_t)x1[u].x;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_tokens(const TokenArgs& a, int dtype, int sm_count, cudaStream_t st) {
+  const int turned = a.rot.axes * a.rot.rot;
+  const bool vec = turned % 8 == 0 && (a.rot.axes == 0 || (a.rot.interleaved ? true : a.rot.rot % 16 == 0));
+  int items;
+  if (vec) items = a.rot.interleaved ? a.head_dim / 8 : turned / 16 + (a.head_dim - turned) / 8;
+  else items = turned / 2 + (a.head_dim - turned);
+  int items_log2 = 0;
+  while ((1 << items_log2) < items) ++items_log2;
+  const int heads = a.q.heads + a.k.heads + a.v.heads;
+  // Blocks of at most kMaxTok tokens; with few tokens the heads are shared out too, until every multiprocessor has two blocks.
+  int per = kMaxTok;
+  while (per > 1 && (int64_t)((a.n + per - 1) / per) < 2 * sm_count) per >>= 1;
+  const int blocks = (a.n + per - 1) / per;
+  int shares = 1;
+  while (blocks * shares < 2 * sm_count && shares * 2 <= heads &&
+         ((int64_t)per * heads << items_log2) / (2 * shares) >= kThreads) shares <<= 1;
+  void* params[3] = {(void*)&a, (void*)&per, (void*)&items_log2};
+  const void* fn;
+  if (dtype == XKV_BF16) fn = vec ? (const void*)tokens_kernel<__nv_bfloat16, true> : (const void*)tokens_kernel<__nv_bfloat16, false>;
+  else fn = vec ? (const void*)tokens_kernel<__half, true> : (const void*)tokens_kernel<__half, false>;
+  const cudaError_t e = launch_overlapped(fn, dim3(blocks, shares), dim3(kThreads), params, 0, st);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace xkv
