@@ -27,7 +27,7 @@ int device_setup(int* device, int* sm_count) {
   if (g_sm_count[dev] == 0) {
     int sms = 0;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return XKV_E_CUDA;
-    if (evict_device_setup() != cudaSuccess) return XKV_E_CUDA;
+    if (evict_device_setup() != cudaSuccess || attn_few_setup() != cudaSuccess) return XKV_E_CUDA;
     g_sm_count[dev] = sms;
   }
   *device = dev;
@@ -57,8 +57,26 @@ bool params_ok(const xkv_paged_params* p) {
   return p->slot_stride >= p->head_dim;
 }
 
-// Workspace: the status word.
-size_t workspace_bytes(const xkv_paged_params*, int) { return 256; }
+// Workspace: the status word, then the scratch of attention for one block per multiprocessor (arrival counts, running
+// maxima and sums, accumulators: two partial results per block).
+struct Layout { size_t off_count, off_ml, off_o, total; };
+Layout make_layout(const xkv_paged_params* p, int sms) {
+  Layout l;
+  size_t off = 256;
+  auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
+  l.off_count = take((size_t)sms * sizeof(unsigned int));
+  l.off_ml = take((size_t)2 * sms * kChunkRows * sizeof(float2));
+  l.off_o = take((size_t)2 * sms * kChunkRows * p->head_dim * sizeof(float));
+  l.total = off;
+  return l;
+}
+
+// Most units of work that the device's numbers could amount to, for counters of 32 bits.
+bool work_ok(const xkv_paged* c, const xkv_paged_batch* b) {
+  const int64_t units = (int64_t)b->table_width * c->p.page_tokens / 128 + 2;
+  const int64_t tiles = (int64_t)b->max_new * c->view.group / (kChunkRows / 2) + 2;
+  return (double)b->n_seqs * c->p.n_kv_heads * (double)units * (double)tiles < 4294967296.0;
+}
 
 bool batch_ok(const xkv_paged* c, const xkv_paged_batch* b, bool tokens) {
   if (!b || b->n_seqs < 1 || b->n_seqs > c->p.max_seqs || b->table_width < 0) return false;
@@ -149,7 +167,7 @@ int xkv_rotary(const xkv_rotary_params* params, int32_t dtype, int32_t head_dim,
 
 size_t xkv_paged_workspace_bytes(const xkv_paged_params* params, int32_t multiprocessors) {
   if (!params_ok(params) || multiprocessors < 1 || multiprocessors > 1024) return 0;
-  return workspace_bytes(params, multiprocessors);
+  return make_layout(params, multiprocessors).total;
 }
 
 int xkv_paged_create(const xkv_paged_params* params, void* k_pages, void* v_pages, float* weights, void* dev_workspace, size_t bytes,
@@ -167,7 +185,8 @@ int xkv_paged_create(const xkv_paged_params* params, void* k_pages, void* v_page
   int dev, sms;
   const int rc = device_setup(&dev, &sms);
   if (rc != XKV_OK) return rc;
-  const size_t need = workspace_bytes(params, sms);
+  const Layout layout = make_layout(params, sms);
+  const size_t need = layout.total;
   if (bytes < need) return XKV_E_NOMEM;
   xkv_paged* c = new (std::nothrow) xkv_paged;
   if (!c) return XKV_E_NOMEM;
@@ -183,6 +202,10 @@ int xkv_paged_create(const xkv_paged_params* params, void* k_pages, void* v_page
   v.n_heads = params->n_heads; v.n_kv_heads = params->n_kv_heads; v.group = params->n_heads / params->n_kv_heads;
   v.page_shift = log2_of(params->page_tokens); v.n_pages = params->n_pages;
   v.status = reinterpret_cast<int*>(c->ws);
+  c->scratch.count = reinterpret_cast<unsigned int*>(c->ws + layout.off_count);
+  c->scratch.ml = reinterpret_cast<float2*>(c->ws + layout.off_ml);
+  c->scratch.o = reinterpret_cast<float*>(c->ws + layout.off_o);
+  if (make_pool_maps(v, params->head_dim, params->dtype, 16, &c->maps16) != cudaSuccess) { delete c; return XKV_E_CUDA; }
   if (cudaMemsetAsync(c->ws, 0, need, reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess) { delete c; return XKV_E_CUDA; }
   *out = c;
   return XKV_OK;
@@ -240,7 +263,12 @@ int attn_paged_causal(xkv_paged* c, const xkv_paged_batch* b, const void* q, int
   a.q = reinterpret_cast<const uint8_t*>(q); a.q_ts = q_ts; a.q_hs = q_hs;
   a.out = reinterpret_cast<uint8_t*>(out); a.o_ts = o_ts; a.o_hs = o_hs;
   a.lse = lse; a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f; a.full = mask == XKV_MASK_FULL;
-  return from_cuda(launch_paged_attn_simple(a, c->p.head_dim, c->p.dtype, reinterpret_cast<cudaStream_t>(stream)));
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (impl == 1) return from_cuda(launch_paged_attn_simple(a, c->p.head_dim, c->p.dtype, st));
+  if (!work_ok(c, b)) return XKV_E_LIMIT;
+  if ((int64_t)b->max_new * c->view.group <= kFewRows)
+    return from_cuda(launch_attn_few(a, c->maps16, c->scratch, c->p.head_dim, c->p.dtype, c->sm_count, st));
+  return from_cuda(launch_paged_attn_simple(a, c->p.head_dim, c->p.dtype, st));
 }
 
 int kv_paged_weights(xkv_paged* c, const xkv_paged_batch* b, const void* q, int64_t q_ts, int64_t q_hs, const float* lse, float scale, float decay,

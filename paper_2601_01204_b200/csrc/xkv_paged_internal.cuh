@@ -112,6 +112,22 @@ struct PagedAttnArgs {
   float scale, scale_log2;
   int full;                              // every token of the sequence is seen
 };
+
+// Tensor maps of the two pools for copies of `rows` token slots by 64 channels (16-byte pieces permuted within 128-byte
+// rows as the matrix operands want them), and scratch: partial results of work that was cut between blocks.
+struct PoolMaps { CUtensorMap k, v; };
+struct PagedScratch {
+  float* o;              // [2 * blocks][rows][head_dim] accumulators
+  float2* ml;            // [2 * blocks][rows] running maximum (log2 units) and sum
+  unsigned int* count;   // [blocks] arrivals at the item that starts in a block and goes on in the next one (0 between calls)
+};
+constexpr int kFewRows = 16;       // rows of the kernel for few rows (a tile of a warp's matrix instruction)
+constexpr int kChunkRows = 256;    // rows of the kernel for chunks (two tiles of tcgen05.mma)
+cudaError_t make_pool_maps(const PagedView& c, int head_dim, int dtype, int rows, PoolMaps* maps);
+cudaError_t attn_few_setup();
+// group * max_new <= kFewRows
+cudaError_t launch_attn_few(const PagedAttnArgs& a, const PoolMaps& maps, const PagedScratch& s, int head_dim, int dtype, int sm_count,
+                            cudaStream_t st);
 cudaError_t launch_paged_attn_simple(const PagedAttnArgs& a, int head_dim, int dtype, cudaStream_t st);
 
 struct PagedWeightArgs {
@@ -130,4 +146,6 @@ struct xkv_paged {
   xkv::PagedView view;
   int sm_count, device;
   uint8_t* ws; size_t ws_bytes;
+  xkv::PagedScratch scratch;
+  xkv::PoolMaps maps16;                  // 16 slots at a time
 };

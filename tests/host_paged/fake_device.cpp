@@ -29,6 +29,9 @@ static cudaError_t launched() { ++g_launches; return cudaSuccess; }
 cudaError_t launch_tokens(const TokenArgs&, int, int, cudaStream_t) { return launched(); }
 cudaError_t launch_evict(const EvictArgs&, cudaStream_t) { return launched(); }
 cudaError_t evict_device_setup() { return cudaSuccess; }
+cudaError_t make_pool_maps(const PagedView&, int, int, int, PoolMaps*) { return cudaSuccess; }
+cudaError_t attn_few_setup() { return cudaSuccess; }
+cudaError_t launch_attn_few(const PagedAttnArgs&, const PoolMaps&, const PagedScratch&, int, int, int, cudaStream_t) { return launched(); }
 cudaError_t launch_paged_attn_simple(const PagedAttnArgs&, int, int, cudaStream_t) { return launched(); }
 cudaError_t launch_paged_weights_simple(const PagedWeightArgs&, int, int, cudaStream_t) { return launched(); }
 }  // namespace xkv
