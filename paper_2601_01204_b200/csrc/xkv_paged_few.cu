@@ -407,25 +407,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
 
 }  // namespace
 
-cudaError_t make_pool_maps(const PagedView& c, int head_dim, int dtype, int rows, PoolMaps* maps) {
-  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult found;
-  cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
-  if (e != cudaSuccess) return e;
-  if (found != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
-  const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)1 << c.page_shift, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
-  const cuuint64_t strides[3] = {(cuuint64_t)c.slot_stride * 2, (cuuint64_t)c.head_stride * 2, (cuuint64_t)c.page_stride * 2};
-  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, one[4] = {1, 1, 1, 1};
-  const CUtensorMapDataType type = dtype == XKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  for (int i = 0; i < 2; ++i)
-    if (reinterpret_cast<Encode>(fn)(i ? &maps->v : &maps->k, type, 4, i ? c.v : c.k, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return cudaErrorInvalidValue;
-  return cudaSuccess;
-}
-
 template <int D, bool BF16>
 static cudaError_t setup_one() {
   return cudaFuncSetAttribute(attn_few_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Few<D>::kBytes);

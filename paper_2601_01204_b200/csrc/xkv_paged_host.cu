@@ -27,7 +27,7 @@ int device_setup(int* device, int* sm_count) {
   if (g_sm_count[dev] == 0) {
     int sms = 0;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return XKV_E_CUDA;
-    if (evict_device_setup() != cudaSuccess || attn_few_setup() != cudaSuccess) return XKV_E_CUDA;
+    if (evict_device_setup() != cudaSuccess || attn_few_setup() != cudaSuccess || attn_chunk_setup() != cudaSuccess) return XKV_E_CUDA;
     g_sm_count[dev] = sms;
   }
   *device = dev;
@@ -59,12 +59,13 @@ bool params_ok(const xkv_paged_params* p) {
 
 // Workspace: the status word, then the scratch of attention for one block per multiprocessor (arrival counts, running
 // maxima and sums, accumulators: two partial results per block).
-struct Layout { size_t off_count, off_ml, off_o, total; };
+struct Layout { size_t off_count, off_cuts, off_ml, off_o, total; };
 Layout make_layout(const xkv_paged_params* p, int sms) {
   Layout l;
   size_t off = 256;
   auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
   l.off_count = take((size_t)sms * sizeof(unsigned int));
+  l.off_cuts = take((size_t)sms * attn_chunk_cut_bytes());
   l.off_ml = take((size_t)2 * sms * kChunkRows * sizeof(float2));
   l.off_o = take((size_t)2 * sms * kChunkRows * p->head_dim * sizeof(float));
   l.total = off;
@@ -205,7 +206,9 @@ int xkv_paged_create(const xkv_paged_params* params, void* k_pages, void* v_page
   c->scratch.count = reinterpret_cast<unsigned int*>(c->ws + layout.off_count);
   c->scratch.ml = reinterpret_cast<float2*>(c->ws + layout.off_ml);
   c->scratch.o = reinterpret_cast<float*>(c->ws + layout.off_o);
-  if (make_pool_maps(v, params->head_dim, params->dtype, 16, &c->maps16) != cudaSuccess) { delete c; return XKV_E_CUDA; }
+  c->cuts = c->ws + layout.off_cuts;
+  if (make_pool_maps(v, params->head_dim, params->dtype, 16, &c->maps16) != cudaSuccess ||
+      make_pool_maps(v, params->head_dim, params->dtype, params->page_tokens < 128 ? params->page_tokens : 128, &c->maps_page) != cudaSuccess) { delete c; return XKV_E_CUDA; }
   if (cudaMemsetAsync(c->ws, 0, need, reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess) { delete c; return XKV_E_CUDA; }
   *out = c;
   return XKV_OK;
@@ -268,7 +271,7 @@ int attn_paged_causal(xkv_paged* c, const xkv_paged_batch* b, const void* q, int
   if (!work_ok(c, b)) return XKV_E_LIMIT;
   if ((int64_t)b->max_new * c->view.group <= kFewRows)
     return from_cuda(launch_attn_few(a, c->maps16, c->scratch, c->p.head_dim, c->p.dtype, c->sm_count, st));
-  return from_cuda(launch_paged_attn_simple(a, c->p.head_dim, c->p.dtype, st));
+  return from_cuda(launch_attn_chunk(a, c->maps_page, c->scratch, c->cuts, c->p.head_dim, c->p.dtype, c->sm_count, st));
 }
 
 int kv_paged_weights(xkv_paged* c, const xkv_paged_batch* b, const void* q, int64_t q_ts, int64_t q_hs, const float* lse, float scale, float decay,

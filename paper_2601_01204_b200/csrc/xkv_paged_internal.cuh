@@ -128,6 +128,14 @@ cudaError_t attn_few_setup();
 // group * max_new <= kFewRows
 cudaError_t launch_attn_few(const PagedAttnArgs& a, const PoolMaps& maps, const PagedScratch& s, int head_dim, int dtype, int sm_count,
                             cudaStream_t st);
+size_t attn_chunk_cut_bytes();
+cudaError_t attn_chunk_setup();
+// Any numbers of new tokens; maps: copies of min(page_tokens, 128) slots; cuts: attn_chunk_cut_bytes() per multiprocessor.
+cudaError_t launch_attn_chunk(const PagedAttnArgs& a, const PoolMaps& maps, const PagedScratch& s, void* cuts, int head_dim, int dtype,
+                              int sm_count, cudaStream_t st);
+// Tensor map of a token tensor: boxes of 64 channels, `heads` heads and `toks` tokens.
+cudaError_t make_token_map(const void* base, int64_t ts, int64_t hs, int n, int n_heads, int head_dim, int dtype, int heads, int toks,
+                           CUtensorMap* map);
 cudaError_t launch_paged_attn_simple(const PagedAttnArgs& a, int head_dim, int dtype, cudaStream_t st);
 
 struct PagedWeightArgs {
@@ -147,5 +155,6 @@ struct xkv_paged {
   int sm_count, device;
   uint8_t* ws; size_t ws_bytes;
   xkv::PagedScratch scratch;
-  xkv::PoolMaps maps16;                  // 16 slots at a time
+  xkv::PoolMaps maps16, maps_page;       // 16 slots at a time, min(page_tokens, 128) slots at a time
+  void* cuts;
 };

@@ -32,6 +32,9 @@ cudaError_t evict_device_setup() { return cudaSuccess; }
 cudaError_t make_pool_maps(const PagedView&, int, int, int, PoolMaps*) { return cudaSuccess; }
 cudaError_t attn_few_setup() { return cudaSuccess; }
 cudaError_t launch_attn_few(const PagedAttnArgs&, const PoolMaps&, const PagedScratch&, int, int, int, cudaStream_t) { return launched(); }
+size_t attn_chunk_cut_bytes() { return 32; }
+cudaError_t attn_chunk_setup() { return cudaSuccess; }
+cudaError_t launch_attn_chunk(const PagedAttnArgs&, const PoolMaps&, const PagedScratch&, void*, int, int, int, cudaStream_t) { return launched(); }
 cudaError_t launch_paged_attn_simple(const PagedAttnArgs&, int, int, cudaStream_t) { return launched(); }
 cudaError_t launch_paged_weights_simple(const PagedWeightArgs&, int, int, cudaStream_t) { return launched(); }
 }  // namespace xkv
