@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libxkv.so")
 SOURCES = ["xkv_host.cu", "xkv_maint.cu", "xkv_attn_simple.cu", "xkv_attn_tc.cu",
            "xkv_paged_host.cu", "xkv_paged_tokens.cu", "xkv_paged_simple.cu", "xkv_paged_evict.cu", "xkv_paged_few.cu",
-           "xkv_paged_chunk.cu", "xkv_paged_maps.cu"]
+           "xkv_paged_chunk.cu", "xkv_paged_maps.cu", "xkv_paged_weights.cu"]
 
 
 def _nvcc() -> str:

@@ -27,7 +27,8 @@ int device_setup(int* device, int* sm_count) {
   if (g_sm_count[dev] == 0) {
     int sms = 0;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return XKV_E_CUDA;
-    if (evict_device_setup() != cudaSuccess || attn_few_setup() != cudaSuccess || attn_chunk_setup() != cudaSuccess) return XKV_E_CUDA;
+    if (evict_device_setup() != cudaSuccess || attn_few_setup() != cudaSuccess || attn_chunk_setup() != cudaSuccess ||
+        weights_setup() != cudaSuccess) return XKV_E_CUDA;
     g_sm_count[dev] = sms;
   }
   *device = dev;
@@ -288,7 +289,8 @@ int kv_paged_weights(xkv_paged* c, const xkv_paged_batch* b, const void* q, int6
   a.cache = c->view; a.seqs = seq_view(b);
   a.q = reinterpret_cast<const uint8_t*>(q); a.q_ts = q_ts; a.q_hs = q_hs;
   a.lse = lse; a.scale_log2 = scale * 1.4426950408889634f; a.decay = decay; a.full = mask == XKV_MASK_FULL;
-  return from_cuda(launch_paged_weights_simple(a, c->p.head_dim, c->p.dtype, reinterpret_cast<cudaStream_t>(stream)));
+  if (!work_ok(c, b)) return XKV_E_LIMIT;
+  return from_cuda(launch_paged_weights(a, c->maps_page, c->p.head_dim, c->p.dtype, c->sm_count, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 int kv_paged_evict(xkv_paged* c, const xkv_paged_batch* b, const int32_t* dst_table, int32_t dst_width, int32_t keep, int32_t n_first,

@@ -145,7 +145,9 @@ struct PagedWeightArgs {
   float scale_log2, decay;
   int full;
 };
-cudaError_t launch_paged_weights_simple(const PagedWeightArgs& a, int head_dim, int dtype, cudaStream_t st);
+cudaError_t weights_setup();
+// maps: as for launch_attn_chunk
+cudaError_t launch_paged_weights(const PagedWeightArgs& a, const PoolMaps& maps, int head_dim, int dtype, int sm_count, cudaStream_t st);
 
 }  // namespace xkv
 

@@ -91,51 +91,7 @@ __global__ void __launch_bounds__(128) paged_attn_simple_kernel(const __grid_con
     a.lse[(int64_t)g * a.seqs.n_tokens + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
-// A thread per cached token and key head.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) paged_weights_simple_kernel(const __grid_constant__ PagedWeightArgs a) {
-  __shared__ float s_q[D];
-  grid_dependency_wait();
-  const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x * 128 + threadIdx.x;
-  const Seq q = seq_at(a.cache, a.seqs, b);
-  if (q.n_new == 0 || (int)(blockIdx.x * 128) >= q.len) return;
-  const int page = j < q.len ? page_at(a.cache, a.seqs.table, a.seqs.table_width, b, j) : -1;
-  const int64_t off = page >= 0 ? 2 * row_offset(a.cache, page, h, j) : -1;
-  float sum = 0.f;
-  for (int i = 0; i < q.n_new; ++i)
-    for (int g = h * a.cache.group; g < (h + 1) * a.cache.group; ++g) {
-      const uint8_t* qp = a.q + 2 * ((int64_t)g * a.q_hs + (int64_t)(q.row0 + i) * a.q_ts);
-      __syncthreads();
-      for (int c = threadIdx.x; c < D / 2; c += 128) {
-        const float2 x = two(*reinterpret_cast<const uint32_t*>(qp + 4 * c), T());
-        s_q[2 * c] = x.x; s_q[2 * c + 1] = x.y;
-      }
-      __syncthreads();
-      if (off < 0 || !(a.full || j < q.len - q.n_new + i + 1)) continue;
-      float d = 0.f;
-      for (int c = 0; c < D / 2; ++c) {
-        const float2 x = two(*reinterpret_cast<const uint32_t*>(a.cache.k + off + 4 * c), T());
-        d = fmaf(s_q[2 * c], x.x, d);
-        d = fmaf(s_q[2 * c + 1], x.y, d);
-      }
-      sum += exp2f(d * a.scale_log2 - a.lse[(int64_t)g * a.seqs.n_tokens + q.row0 + i] * 1.4426950408889634f);
-    }
-  if (page < 0) return;
-  float* w = a.cache.weights + weight_offset(a.cache, page, h, j);
-  *w = (a.decay == 0.f ? 0.f : a.decay * *w) + sum;
-}
-
 }  // namespace
-
-cudaError_t launch_paged_weights_simple(const PagedWeightArgs& a, int head_dim, int dtype, cudaStream_t st) {
-  const void* fn;
-  if (dtype == XKV_BF16) fn = head_dim == 64 ? (const void*)paged_weights_simple_kernel<__nv_bfloat16, 64> : (const void*)paged_weights_simple_kernel<__nv_bfloat16, 128>;
-  else fn = head_dim == 64 ? (const void*)paged_weights_simple_kernel<__half, 64> : (const void*)paged_weights_simple_kernel<__half, 128>;
-  void* params[1] = {(void*)&a};
-  const unsigned tiles = (unsigned)((((int64_t)a.seqs.table_width << a.cache.page_shift) + 127) / 128);
-  const cudaError_t e = launch_overlapped(fn, dim3(tiles, a.cache.n_kv_heads, a.seqs.n_seqs), dim3(128), params, 0, st);
-  return e != cudaSuccess ? e : cudaGetLastError();
-}
 
 cudaError_t launch_paged_attn_simple(const PagedAttnArgs& a, int head_dim, int dtype, cudaStream_t st) {
   const void* fn;

@@ -36,5 +36,6 @@ size_t attn_chunk_cut_bytes() { return 32; }
 cudaError_t attn_chunk_setup() { return cudaSuccess; }
 cudaError_t launch_attn_chunk(const PagedAttnArgs&, const PoolMaps&, const PagedScratch&, void*, int, int, int, cudaStream_t) { return launched(); }
 cudaError_t launch_paged_attn_simple(const PagedAttnArgs&, int, int, cudaStream_t) { return launched(); }
-cudaError_t launch_paged_weights_simple(const PagedWeightArgs&, int, int, cudaStream_t) { return launched(); }
+cudaError_t weights_setup() { return cudaSuccess; }
+cudaError_t launch_paged_weights(const PagedWeightArgs&, const PoolMaps&, int, int, int, cudaStream_t) { return launched(); }
 }  // namespace xkv
