@@ -6,13 +6,16 @@
 // then owns a token and adds its weights up in registers; nothing is exchanged between lanes, and the sums have a fixed order.
 // K is read once, stays in shared memory for all query tiles; the query tiles come from the L2 again for every unit.
 //
-// One block, 20 warps: 16 exponential warps in four groups (a group is four warps, one per quarter of the lanes), one MMA issuer,
-// one for copies, one that stages -lse per column, one idle.  Of a tile of 128 columns each group takes 32, and at the
-// end of a unit the groups' sums meet in shared memory.  FEW: at most 32 rows per sequence and key head (single tokens): a
-// group takes a whole unit, four units are in flight, and nothing has to meet.
+// An item is two units (256 tokens) of a head.  Each query tile that is fetched meets both: with one unit the tiles came from
+// the L2 at 7.4 TB/s, and nothing else mattered (a frame over 16384 tokens 102 us, 65 without the exponentials).
 //
-// What bounds it: with many rows the exponentials (16 per clock and multiprocessor; the MMAs need a quarter to a half of that time),
-// with few rows reading K.
+// One block, 20 warps: 16 exponential warps in four groups (a group is four warps, one per quarter of the lanes), one MMA issuer,
+// one for copies, two that stage -lse per column.  A group has a unit of the item and every second tile, with a buffer of
+// scores of its own (2 units x 2 parities x 128 columns are all of tensor memory); at the item's end the two parities meet in shared
+// memory.  (Half of the columns of every tile instead: 113 us for the frame; what a warp does per tile besides its exponentials counts.)
+//
+// What bounds it: with many rows the exponentials (16 per clock and multiprocessor; a quarter of them are polynomials on the FMA
+// pipes; the MMAs need a quarter to a half of that time), with few rows reading K.
 #include "xkv_paged_line.cuh"
 #include "xkv_ptx.cuh"
 
@@ -21,15 +24,21 @@ namespace xkv {
 namespace {
 
 constexpr int kThreads = 640;
-constexpr int kEW = 16;                       // exponential warps; 16: MMA, 17: copies, 18: lse
+constexpr int kEW = 16;                       // exponential warps; 16: MMA, 17: copies, 18, 19: lse
 constexpr uint32_t kSpinLimit = 1u << 22;
+constexpr int kLse = 4;                       // staged tiles of -lse
+// Places where the parities of an item meet.  The group that adds them up does so before it leaves the item's last tile L, whose -lse is
+// replaced only then.  So its neighbour of the same parity stays before L + 4, the MMAs, which come in order, before L + 6, the
+// groups of the other parity that have scores to read before L + 7, and those that have none (causal) before L + 11, by their own
+// -lse.  Items that meet have two tiles at least: the eighth of them after this one begins at L + 15.
+constexpr int kSums = 8;
 
 template <int D> struct Weigh {
   static constexpr int kSlabs = D / 64;
-  static constexpr int kTile = kSlabs * 16384;
-  static constexpr int kNK = D == 64 ? 6 : 3, kNQ = D == 64 ? 4 : 3;
-  static constexpr int kOffQ = kNK * kTile, kOffBar = kOffQ + kNQ * kTile;
-  static constexpr int kOffLse = kOffBar + 512, kOffSum = kOffLse + 4 * 512, kOffSeq = kOffSum + 2 * 4 * 512;
+  static constexpr int kTile = kSlabs * 16384;               // 128 rows
+  static constexpr int kNK = D == 64 ? 3 : 2, kNQ = D == 64 ? 4 : 2;
+  static constexpr int kOffQ = kNK * 2 * kTile, kOffBar = kOffQ + kNQ * kTile;
+  static constexpr int kOffLse = kOffBar + 512, kOffSum = kOffLse + kLse * 512, kOffSeq = kOffSum + kSums * 2 * 512;
   static constexpr int kOffPrefix = kOffSeq + kMaxSeqs * 12;
   static constexpr size_t kBytes = kOffPrefix + (kMaxSeqs + 1) * 4 + 1024;
 };
@@ -39,25 +48,41 @@ struct WeighArgs {
   int tpt, box_rows;
 };
 
-// Units of the block: every gridDim.x-th of the line.
-struct UnitWalk {
+// Items of the block: every gridDim.x-th of the line.
+struct ItemWalk {
   uint32_t pos, total, step;
-  int seq, head, first;                  // first token of the unit
-  int row0, n_new, len;
-  int tile0, tiles;                      // query tiles that see a token of the unit
+  uint32_t rel, per, seq_end;            // item of the head, items of a head, where the sequence ends on the line
+  int seq, head, first;                  // first token of the item
+  int row0, n_new, len, all_tiles;
+  int tile0, tiles;                      // query tiles that see a token of the item
+  int skip;                              // of them those that see none of its second unit
   __device__ __forceinline__ bool next(const WeighArgs& f, const uint32_t* prefix, const Seq* seqs) {
     if (pos >= total) return false;
-    seq = line_seq(prefix, f.a.seqs.n_seqs, pos);
-    const Seq q = seqs[seq];
-    row0 = q.row0; n_new = q.n_new; len = q.len;
-    const uint32_t per = (uint32_t)((q.len + kUnit - 1) / kUnit), rel = pos - prefix[seq];
-    head = (int)(rel / per);
-    first = (int)(rel - (uint32_t)head * per) * kUnit;
-    // new token i sees slot j iff i >= j - (len - n_new)
-    tile0 = f.a.full ? 0 : max(0, first - (len - n_new)) / f.tpt;
-    tiles = (n_new + f.tpt - 1) / f.tpt - tile0;
+    if (pos >= seq_end) {
+      seq = line_seq(prefix, f.a.seqs.n_seqs, pos);
+      const Seq q = seqs[seq];
+      row0 = q.row0; n_new = q.n_new; len = q.len;
+      seq_end = prefix[seq + 1];
+      per = (uint32_t)((q.len + 2 * kUnit - 1) / (2 * kUnit));
+      rel = pos - prefix[seq];
+      head = (int)(rel / per);
+      rel -= (uint32_t)head * per;
+      all_tiles = (n_new + f.tpt - 1) / f.tpt;
+    } else {                             // (without a division per item and warp)
+      rel += step;
+      if (rel >= 4 * per) { const uint32_t h = rel / per; head += (int)h; rel -= h * per; }
+      while (rel >= per) { rel -= per; ++head; }
+    }
+    first = (int)rel * 2 * kUnit;
+    tile0 = first_tile(f, first);
+    tiles = all_tiles - tile0;
+    skip = first + kUnit < len ? first_tile(f, first + kUnit) - tile0 : tiles;
     pos += step;
     return true;
+  }
+  // new token i sees slot j iff i >= j - (len - n_new)
+  __device__ __forceinline__ int first_tile(const WeighArgs& f, int slot) const {
+    return f.a.full || slot <= len - n_new ? 0 : (slot - (len - n_new)) / f.tpt;
   }
 };
 
@@ -80,7 +105,7 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int
         "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])      \
       : "r"(taddr) : "memory")
 
-template <int D, bool BF16, bool FEW>
+template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1)
 weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ PoolMaps maps, const __grid_constant__ CUtensorMap q_map) {
   using C = Weigh<D>;
@@ -91,13 +116,14 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
   uint8_t* sgen = smem_raw + (sbase - smem_u32(smem_raw));
   const uint32_t sK = sbase, sQ = sbase + C::kOffQ;
   const uint32_t b_kfull = sbase + C::kOffBar, b_kfree = b_kfull + 8 * kNK, b_qfull = b_kfree + 8 * kNK, b_qfree = b_qfull + 8 * kNQ;
-  const uint32_t b_sfull = b_qfree + 8 * kNQ, b_sfree = b_sfull + 32, b_lfull = b_sfree + 32;      // [4] buffers of scores
-  static_assert(8 * (2 * kNK + 2 * kNQ + 12) <= 512 - 16, "barriers");
+  const uint32_t b_sfull = b_qfree + 8 * kNQ, b_sfree = b_sfull + 32;       // [4]: unit + 2 * parity of the tile
+  const uint32_t b_lfull = b_sfree + 32, b_lfree = b_lfull + 8 * kLse, b_sums = b_lfree + 8 * kLse;      // [kLse], [kLse], [kSums][2 units]
+  static_assert(8 * (2 * kNK + 2 * kNQ + 8 + 2 * kLse + 2 * kSums) <= 512 - 16, "barriers");
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 496);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sgen + C::kOffBar + 500);
   const WaitCtx wc{sbase + C::kOffBar + 500};
-  float* s_lse = reinterpret_cast<float*>(sgen + C::kOffLse);        // [4][128] -lse in log2 units
-  float* s_sum = reinterpret_cast<float*>(sgen + C::kOffSum);        // [2][4][128]
+  float* s_lse = reinterpret_cast<float*>(sgen + C::kOffLse);        // [kLse][128] -lse in log2 units
+  float* s_sum = reinterpret_cast<float*>(sgen + C::kOffSum);        // [kSums][2][128]
   Seq* seqs = reinterpret_cast<Seq*>(sgen + C::kOffSeq);
   uint32_t* prefix = reinterpret_cast<uint32_t*>(sgen + C::kOffPrefix);
   __shared__ uint32_t s_warp[kThreads / 32];
@@ -108,7 +134,9 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
     *abort_flag = 0;
     for (int i = 0; i < kNK; ++i) { mbar_init(b_kfull + 8 * i, 1); mbar_init(b_kfree + 8 * i, 1); }
     for (int i = 0; i < kNQ; ++i) { mbar_init(b_qfull + 8 * i, 1); mbar_init(b_qfree + 8 * i, 1); }
-    for (int i = 0; i < 4; ++i) { mbar_init(b_sfull + 8 * i, 1); mbar_init(b_sfree + 8 * i, FEW ? 4 : kEW); mbar_init(b_lfull + 8 * i, 32); }
+    for (int i = 0; i < 4; ++i) { mbar_init(b_sfull + 8 * i, 1); mbar_init(b_sfree + 8 * i, 4); }
+    for (int i = 0; i < kLse; ++i) { mbar_init(b_lfull + 8 * i, 32); mbar_init(b_lfree + 8 * i, 8); }
+    for (int i = 0; i < 2 * kSums; ++i) mbar_init(b_sums + 8 * i, 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kEW) {
@@ -119,112 +147,145 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
   line_prefix<kThreads>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {
     const Seq q = seq_at(a.cache, a.seqs, s);
     seqs[s] = q;
-    return q.n_new == 0 ? 0u : (uint32_t)a.cache.n_kv_heads * (uint32_t)((q.len + kUnit - 1) / kUnit);
+    return q.n_new == 0 ? 0u : (uint32_t)a.cache.n_kv_heads * (uint32_t)((q.len + 2 * kUnit - 1) / (2 * kUnit));
   });
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-  UnitWalk walk;
+  ItemWalk walk;
   walk.pos = blockIdx.x;
   walk.step = gridDim.x;
   walk.total = prefix[a.seqs.n_seqs];
+  walk.seq_end = 0;
   const int G = a.cache.group;
 
   if (warp < kEW) {
-    // ============== exponentials: thread = token of the unit ==============
-    const int group = warp >> 2;
+    // ============== exponentials: thread = token of a unit ==============
+    const uint32_t u = warp >> 3;                          // unit of the item
+    const uint32_t odd = (warp >> 2) & 1;                  // parity of the tiles
     const int key = (warp & 3) * 32 + lane;
-    const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t buf = u + 2 * odd, scores = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 128 * buf;
     const uint64_t sc2 = pack_f2(a.scale_log2, a.scale_log2);
-    uint32_t cnt = 0;                       // tiles so far, of all groups
-    for (uint32_t unit = 0; walk.next(f, prefix, seqs); ++unit) {
-      // the unit's old weights and their places, for the group that will write them
-      const bool mine = (unit & 3) == (uint32_t)group;
+    uint32_t cnt = 0, ph = 0;                // tiles of the block so far; phase of this group's buffer
+    uint32_t sum_at = 0, sum_ph = 0;         // place where the next item's parities meet, and its phase
+    for (; walk.next(f, prefix, seqs); cnt += (uint32_t)walk.tiles) {
+      const int token = walk.first + kUnit * (int)u + key;
+      const int from = u ? walk.skip : 0;                    // the unit's first tile
+      const bool writes = ((cnt + (uint32_t)walk.tiles - 1) & 1) == odd;       // the item's last tile is this group's
+      // the old weight and its place, asked for here and looked at after the group's first tile
+      const bool in = writes && token < walk.len;
+      int page = -1;
+      if (in) page = a.seqs.table[(int64_t)walk.seq * a.seqs.table_width + (token >> a.cache.page_shift)];
       float* place = nullptr;
-      float old = 0.f;
-      if (mine && walk.first + key < walk.len) {
-        const int page = page_at(a.cache, a.seqs.table, a.seqs.table_width, walk.seq, walk.first + key);
-        if (page >= 0) {
-          place = a.cache.weights + weight_offset(a.cache, page, walk.head, walk.first + key);
-          if (a.decay != 0.f) old = *place;
-        }
-      }
-      float total = 0.f;
-      const int base = walk.len - walk.n_new;                 // token i sees slots <= base + i
-      for (int j = 0; j < walk.tiles; ++j, ++cnt) {
-        if (FEW && !mine) continue;
-        const uint32_t buf = cnt & 3, ph = (cnt >> 2) & 1;
+      float old = 0.f, total = 0.f;
+      const int base = walk.len - walk.n_new;                // token i sees slots <= base + i
+      const int j0 = (int)((odd - cnt) & 1);
+      for (int j = j0; j < walk.tiles; j += 2) {
+        const uint32_t at = (cnt + (uint32_t)j) % kLse;
         const int tok0 = (walk.tile0 + j) * f.tpt;
         const int cols = min(f.tpt, walk.n_new - tok0) * G;
-        const int c0 = FEW ? 0 : 32 * group;
-        mbar_wait(b_sfull + 8 * buf, ph, wc);
-        mbar_wait(b_lfull + 8 * buf, ph, wc);
-        __syncwarp();
-        tc_fence_after();
-        if (c0 < cols) {
-          uint32_t s[32];
-          XKV_TMEM_LD_32(lane_addr + 128 * buf + c0, s);
-          tc_wait_ld();
-          const float4* nl = reinterpret_cast<const float4*>(s_lse + 128 * buf + c0);
-          // columns that see the token: tokens i >= slot - base; columns behind the tile's rows belong to nobody
-          const int lo = a.full ? 0 : (walk.first + key - base - tok0) * G - c0, hi = cols - c0;
-          uint64_t sum = 0ull;
-          const bool plain = hi >= 32 && (a.full || walk.first + kUnit - 1 <= base + tok0);      // (the same in all threads)
-          if (plain) {
+        mbar_wait(b_lfull + 8 * at, ((cnt + (uint32_t)j) / kLse) & 1, wc);
+        if (j >= from) {
+          mbar_wait(b_sfull + 8 * buf, ph, wc);
+          ph ^= 1;
+          __syncwarp();
+          tc_fence_after();
+          // columns [lo, cols) see the token: tokens i >= token - base; columns behind the tile's rows belong to nobody
+          const int lo = a.full ? 0 : (token - base - tok0) * G;
+          const bool all = a.full || walk.first + kUnit * (int)u + kUnit - 1 <= base + tok0;      // (the same in all threads)
+          uint64_t sum = 0ull, sum1 = 0ull;
+#pragma unroll 1
+          for (int c0 = 0; c0 < cols; c0 += 32) {
+            uint32_t s[32];
+            XKV_TMEM_LD_32(scores + c0, s);
+            tc_wait_ld();
+            const float4* nl = reinterpret_cast<const float4*>(s_lse + 128 * at + c0);
+            if (all && c0 + 32 <= cols) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float4 n = nl[i];
-              const uint64_t x0 = fma_f2(pack_f2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), sc2, pack_f2(n.x, n.y));
-              const uint64_t x1 = fma_f2(pack_f2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), sc2, pack_f2(n.z, n.w));
-              sum = add_f2(sum, pack_f2(fast_exp2(f2_lo(x0)), fast_exp2(f2_hi(x0))));
-              sum = add_f2(sum, pack_f2(fast_exp2(f2_lo(x1)), fast_exp2(f2_hi(x1))));
-            }
-          } else {
+              for (int i = 0; i < 8; ++i) {
+                const float4 n = nl[i];
+                const uint64_t x0 = fma_f2(pack_f2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), sc2, pack_f2(n.x, n.y));
+                const uint64_t x1 = fma_f2(pack_f2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), sc2, pack_f2(n.z, n.w));
+                sum = add_f2(sum, pack_f2(fast_exp2(f2_lo(x0)), fast_exp2(f2_hi(x0))));
+                sum1 = add_f2(sum1, (i & 1) ? exp2_pair<5>(x1) : pack_f2(fast_exp2(f2_lo(x1)), fast_exp2(f2_hi(x1))));
+              }
+            } else {
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const float2 n = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(nl) + i);
-              const float p0 = fast_exp2(fmaf(__uint_as_float(s[i]), a.scale_log2, n.x)), p1 = fast_exp2(fmaf(__uint_as_float(s[i + 1]), a.scale_log2, n.y));
-              sum = add_f2(sum, pack_f2(i >= lo && i < hi ? p0 : 0.f, i + 1 >= lo && i + 1 < hi ? p1 : 0.f));
+              for (int i = 0; i < 32; i += 2) {
+                const float2 n = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(nl) + i);
+                const float p0 = fast_exp2(fmaf(__uint_as_float(s[i]), a.scale_log2, n.x)), p1 = fast_exp2(fmaf(__uint_as_float(s[i + 1]), a.scale_log2, n.y));
+                sum = add_f2(sum, pack_f2(c0 + i >= lo && c0 + i < cols ? p0 : 0.f, c0 + i + 1 >= lo && c0 + i + 1 < cols ? p1 : 0.f));
+              }
             }
           }
-          total += f2_lo(sum) + f2_hi(sum);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_sfree + 8 * buf);
+          total += (f2_lo(sum) + f2_hi(sum)) + (f2_lo(sum1) + f2_hi(sum1));
         }
-        tc_fence_before();
+        if (in && !place) {
+          if ((unsigned)page < (unsigned)a.cache.n_pages) {
+            place = a.cache.weights + weight_offset(a.cache, page, walk.head, token);
+            if (a.decay != 0.f) old = *place;
+          } else {
+            paged_report(a.cache.status, (int)XKV_E_INVALID);
+          }
+        }
+        if (j == walk.tiles - 1) {
+          if (walk.tiles > 1) {
+            mbar_wait(b_sums + 8 * (2 * sum_at + u), sum_ph, wc);
+            __syncwarp();
+            total += s_sum[(2 * sum_at + u) * 128 + key];
+          }
+          if (place) *place = a.decay * old + total;
+        }
         __syncwarp();
-        if (lane == 0) mbar_arrive(b_sfree + 8 * buf);
+        if (lane == 0) mbar_arrive(b_lfree + 8 * at);
       }
-      if (!FEW) {
-        float* sums = s_sum + (unit & 1) * 512;
-        sums[group * 128 + key] = total;
-        asm volatile("bar.sync 1, 512;" ::: "memory");
-        if (mine) total = (sums[key] + sums[128 + key]) + (sums[256 + key] + sums[384 + key]);
+      if (walk.tiles > 1) {
+        if (!writes) {
+          s_sum[(2 * sum_at + u) * 128 + key] = total;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_sums + 8 * (2 * sum_at + u));
+        }
+        if (++sum_at == kSums) { sum_at = 0; sum_ph ^= 1; }
       }
-      if (place) *place = a.decay * old + total;
     }
     tc_fence_before();
   } else if (warp == kEW) {
     // =========================== MMA issuer ===================================
     const uint64_t dk0 = make_desc(sK), dq0 = make_desc(sQ);
     uint32_t kb = 0, kph = 0, qb = 0, qph = 0, cnt = 0;
+    uint32_t par = 0, used = 0;              // of the four buffers: phases, and whether they have held scores
     while (walk.next(f, prefix, seqs)) {
       mbar_wait(b_kfull + 8 * kb, kph, wc);
       for (int j = 0; j < walk.tiles; ++j, ++cnt) {
-        const uint32_t buf = cnt & 3;
         const int cols = min(f.tpt, walk.n_new - (walk.tile0 + j) * f.tpt) * G;
+        const uint32_t idesc = make_idesc((cols + 15) & ~15, BF16, false);
+        const uint64_t dq = dq0 + (uint64_t)(qb * (kTile >> 4));
         mbar_wait(b_qfull + 8 * qb, qph, wc);
-        if (cnt >= 4) mbar_wait(b_sfree + 8 * buf, ((cnt >> 2) - 1) & 1, wc);
-        __syncwarp();
-        tc_fence_after();
-        if (elect_one()) {
-          const uint32_t idesc = make_idesc((cols + 15) & ~15, BF16, false);
-          const uint64_t dk = dk0 + (uint64_t)(kb * (kTile >> 4)), dq = dq0 + (uint64_t)(qb * (kTile >> 4));
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint64_t at = (uint64_t)((ks >> 2) * (16384 >> 4) + (ks & 3) * 2);
-            mma_ss(tmem + 128 * buf, dk + at, dq + at, idesc, ks > 0 ? 1u : 0u);
+        for (uint32_t u = 0; u < 2; ++u) {
+          if (u && j < walk.skip) break;
+          const uint32_t buf = u + 2 * (cnt & 1);
+          if ((used >> buf) & 1) mbar_wait(b_sfree + 8 * buf, ((par >> buf) & 1) ^ 1, wc);
+          used |= 1u << buf;
+          par ^= 1u << buf;
+          __syncwarp();
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t dk = dk0 + (uint64_t)((2 * kb + u) * (kTile >> 4));
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint64_t at = (uint64_t)((ks >> 2) * (16384 >> 4) + (ks & 3) * 2);
+              mma_ss(tmem + 128 * buf, dk + at, dq + at, idesc, ks > 0 ? 1u : 0u);
+            }
+            tc_commit(b_sfull + 8 * buf);
           }
-          tc_commit(b_sfull + 8 * buf);
+          __syncwarp();
+        }
+        if (elect_one()) {
           tc_commit(b_qfree + 8 * qb);
           if (j == walk.tiles - 1) tc_commit(b_kfree + 8 * kb);
         }
@@ -237,23 +298,23 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
   } else if (warp == kEW + 1) {
     // =========================== copies =======================================
     const int page_mask = (1 << a.cache.page_shift) - 1;
-    const int per_unit = kUnit / f.box_rows;
+    const int per_item = 2 * kUnit / f.box_rows;          // copies, 2..16
     uint32_t g = 0, gq = 0;
-    auto pages = [&](const UnitWalk& w) {                 // of a unit's copies, one per lane; none: outside the map
+    auto pages = [&](const ItemWalk& w) {                 // of an item's copies, one per lane; none: outside the map
       const int slot = w.first + lane * f.box_rows;
-      const int p = lane < per_unit && slot < w.len ? page_at(a.cache, a.seqs.table, a.seqs.table_width, w.seq, slot) : -1;
+      const int p = lane < per_item && slot < w.len ? page_at(a.cache, a.seqs.table, a.seqs.table_width, w.seq, slot) : -1;
       return p < 0 ? a.cache.n_pages : p;
     };
-    UnitWalk ahead = walk;
+    ItemWalk ahead = walk;
     bool more = ahead.next(f, prefix, seqs);
     int ids = more ? pages(ahead) : 0;
     while (more) {
-      const UnitWalk w = ahead;
+      const ItemWalk w = ahead;
       const int now = ids;
       more = ahead.next(f, prefix, seqs);
-      if (more) ids = pages(ahead);                       // (the next unit's look-ups run beside this one's copies)
+      if (more) ids = pages(ahead);                       // (the next item's look-ups run beside this one's copies)
       const uint32_t ks = g % kNK;
-      const int boxes = min(per_unit, (w.len - w.first + f.box_rows - 1) / f.box_rows);
+      const int boxes = min(per_item, (w.len - w.first + f.box_rows - 1) / f.box_rows);
       mbar_wait<500>(b_kfree + 8 * ks, ((g / kNK) & 1) ^ 1, wc);
       __syncwarp();
       if (lane == 0) mbar_expect_tx(b_kfull + 8 * ks, (uint32_t)(boxes * f.box_rows * 128 * kSlabs));
@@ -262,12 +323,13 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
         if (lane == 0)
 #pragma unroll
           for (int c = 0; c < kSlabs; ++c)
-            tma_4d(sK + ks * kTile + c * 16384 + i * f.box_rows * 128, &maps.k, 64 * c, (w.first + i * f.box_rows) & page_mask, w.head, page, b_kfull + 8 * ks);
+            tma_4d(sK + (2 * ks + (i * f.box_rows) / kUnit) * kTile + c * 16384 + ((i * f.box_rows) & (kUnit - 1)) * 128, &maps.k, 64 * c,
+                   (w.first + i * f.box_rows) & page_mask, w.head, page, b_kfull + 8 * ks);
       }
       ++g;
       for (int j = 0; j < w.tiles; ++j, ++gq) {
         const uint32_t qs = gq % kNQ;
-        mbar_wait<200>(b_qfree + 8 * qs, ((gq / kNQ) & 1) ^ 1, wc);
+        mbar_wait(b_qfree + 8 * qs, ((gq / kNQ) & 1) ^ 1, wc);
         __syncwarp();
         if (lane == 0) {
           mbar_expect_tx(b_qfull + 8 * qs, (uint32_t)(kSlabs * 128 * f.tpt * G));
@@ -290,31 +352,55 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
       drain(b_qfull, kNQ, gq);
     }
     __syncwarp();
-  } else if (warp == kEW + 2) {
+  } else {
     // =========================== -lse of a tile's columns =====================
-    uint32_t cnt = 0;
-    while (walk.next(f, prefix, seqs)) {
-      for (int j = 0; j < walk.tiles; ++j, ++cnt) {
-        const uint32_t buf = cnt & 3;
-        const int tok0 = (walk.tile0 + j) * f.tpt;
-        const int cols = min(f.tpt, walk.n_new - tok0) * G;
-        float x[4];
+    // Two warps take turns; each asks for the values of its next tile before it hands over those of this one, so that their way
+    // from memory is never waited for (one warp, one tile at a time: 246 us for a frame over 16384 tokens instead of 109).
+    int64_t off[4];                         // of this lane's columns: place after the tile's first value
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c = lane + 32 * i;
-          x[i] = -INFINITY;
-          if (c < cols) {
-            const int tok = c / G;
-            const float v = a.lse[(int64_t)(walk.head * G + (c - tok * G)) * a.seqs.n_tokens + walk.row0 + tok0 + tok];
-            x[i] = v == -INFINITY ? v : -v * 1.4426950408889634f;        // (a row that saw nothing gives nothing)
-          }
-        }
-        if (cnt >= 4) mbar_wait<100>(b_sfree + 8 * buf, ((cnt >> 2) - 1) & 1, wc);
-        __syncwarp();
+    for (int i = 0; i < 4; ++i) {
+      const int c = lane + 32 * i, tok = c / G;
+      off[i] = (int64_t)(c - tok * G) * a.seqs.n_tokens + tok;
+    }
+    int j = -1;
+    bool live = walk.next(f, prefix, seqs);
+    uint32_t cnt = 0xffffffffu;             // the tile at hand
+    auto advance = [&]() {                  // to the next tile of the block
+      if (!live) return;
+      ++cnt;
+      if (++j == walk.tiles) { j = 0; live = walk.next(f, prefix, seqs); }
+    };
+    auto fetch = [&](float (&x)[4]) {
+      const int tok0 = (walk.tile0 + j) * f.tpt;
+      const int cols = min(f.tpt, walk.n_new - tok0) * G;
+      const float* src = a.lse + (int64_t)walk.head * G * a.seqs.n_tokens + walk.row0 + tok0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s_lse[128 * buf + lane + 32 * i] = x[i];
-        mbar_arrive(b_lfull + 8 * buf);
-      }
+      for (int i = 0; i < 4; ++i) x[i] = lane + 32 * i < cols ? src[off[i]] : -INFINITY;
+    };
+    auto put = [&](uint32_t now, const float (&x)[4]) {
+      const uint32_t at = now % kLse;
+      if (now >= (uint32_t)kLse) mbar_wait(b_lfree + 8 * at, ((now / kLse) - 1) & 1, wc);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)           // (a row that saw nothing, lse -inf, gives nothing)
+        s_lse[128 * at + lane + 32 * i] = x[i] == -INFINITY ? x[i] : -x[i] * 1.4426950408889634f;
+      mbar_arrive(b_lfull + 8 * at);
+    };
+    float x[4], y[4];
+    for (int i = 0; i <= warp - (kEW + 2); ++i) advance();
+    if (live) fetch(x);
+    while (live) {
+      uint32_t now = cnt;
+      advance();
+      advance();
+      if (live) fetch(y);
+      put(now, x);
+      if (!live) break;
+      now = cnt;
+      advance();
+      advance();
+      if (live) fetch(x);
+      put(now, y);
     }
   }
   __syncthreads();
@@ -328,13 +414,7 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
 
 template <int D, bool BF16>
 cudaError_t setup_one() {
-  const cudaError_t e = cudaFuncSetAttribute(weights_kernel<D, BF16, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Weigh<D>::kBytes);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(weights_kernel<D, BF16, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Weigh<D>::kBytes);
-}
-
-template <int D, bool BF16>
-const void* kernel_of(bool few) {
-  return few ? (const void*)weights_kernel<D, BF16, true> : (const void*)weights_kernel<D, BF16, false>;
+  return cudaFuncSetAttribute(weights_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Weigh<D>::kBytes);
 }
 
 }  // namespace
@@ -355,12 +435,12 @@ cudaError_t launch_paged_weights(const PagedWeightArgs& a, const PoolMaps& maps,
   CUtensorMap q_map;
   cudaError_t e = make_token_map(a.q, a.q_ts, a.q_hs, a.seqs.n_tokens, a.cache.n_heads, head_dim, dtype, a.cache.group, f.tpt, &q_map);
   if (e != cudaSuccess) return e;
-  const bool few = (int64_t)a.seqs.max_new * a.cache.group <= 32, bf16 = dtype == XKV_BF16;
-  const int64_t most = (int64_t)a.seqs.n_seqs * a.cache.n_kv_heads * ((((int64_t)a.seqs.table_width << a.cache.page_shift) + kUnit - 1) / kUnit);
+  const bool bf16 = dtype == XKV_BF16;
+  const int64_t most = (int64_t)a.seqs.n_seqs * a.cache.n_kv_heads * ((((int64_t)a.seqs.table_width << a.cache.page_shift) + 2 * kUnit - 1) / (2 * kUnit));
   const unsigned grid = (unsigned)(most < sm_count ? most : sm_count);
   const void* fn;
-  if (head_dim == 64) fn = bf16 ? kernel_of<64, true>(few) : kernel_of<64, false>(few);
-  else fn = bf16 ? kernel_of<128, true>(few) : kernel_of<128, false>(few);
+  if (head_dim == 64) fn = bf16 ? (const void*)weights_kernel<64, true> : (const void*)weights_kernel<64, false>;
+  else fn = bf16 ? (const void*)weights_kernel<128, true> : (const void*)weights_kernel<128, false>;
   void* p[3] = {(void*)&f, (void*)&maps, (void*)&q_map};
   e = launch_overlapped(fn, dim3(grid), dim3(kThreads), p, head_dim == 64 ? Weigh<64>::kBytes : Weigh<128>::kBytes, st);
   return e != cudaSuccess ? e : cudaGetLastError();
