@@ -38,7 +38,7 @@ template <int D> struct Chunk {
   static constexpr int kTile = kSlabs * 16384;
   static constexpr int kNK = D == 64 ? 4 : 2, kNV = D == 64 ? 4 : 2;
   static constexpr int kOffK = 2 * kTile, kOffV = kOffK + kNK * kTile, kOffBar = kOffV + kNV * kTile;
-  static constexpr int kBars = 2 * kNK + 3 * kNV + 2 + 2 + 2 + 2 + 4 + 4 + 2;
+  static constexpr int kBars = 2 * kNK + 3 * kNV + 2 + 2 + 2 + 2 + 4 + 4 + 2 + 4;
   static constexpr int kOffPrefix = kOffBar + 512;
   static constexpr size_t kBytes = kOffPrefix + (kMaxSeqs + 1) * 4 + 1024;
   // tensor memory columns
@@ -148,6 +148,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
   // [2 tiles][2], even and odd steps: P V done, P written (the warps of a tile may be almost a step apart)
   const uint32_t b_pvdone = b_sfree + 16, b_pfull = b_pvdone + 32, b_ofree = b_pfull + 32;
   const uint32_t b_vfix = b_ofree + 16;       // [kNV], one per stage: a stage is not filled again before both tiles have passed it
+  const uint32_t b_phalf = b_vfix + 8 * kNV;  // [2 tiles][2] head_dim 128: P of the unit's first 64 tokens written
   static_assert(8 * C::kBars <= 512 - 16, "barriers");
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 496);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sgen + C::kOffBar + 500);
@@ -166,6 +167,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       mbar_init(b_sfree + 8 * t, kRowThreads); mbar_init(b_ofree + 8 * t, kRowThreads);
       mbar_init(b_pvdone + 16 * t, 1); mbar_init(b_pvdone + 16 * t + 8, 1);
       mbar_init(b_pfull + 16 * t, kRowThreads); mbar_init(b_pfull + 16 * t + 8, kRowThreads);
+      mbar_init(b_phalf + 16 * t, kRowThreads); mbar_init(b_phalf + 16 * t + 8, kRowThreads);
     }
     for (int i = 0; i < kNV; ++i) mbar_init(b_vfix + 8 * i, 32);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -200,7 +202,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32 + 16 * (warp >> 3)) << 16);
     const uint32_t col_t = lane_addr + C::kColTile * t;
     const uint32_t colO = lane_addr + C::kColO + D * t;
-    const uint32_t sfull = b_sfull + 8 * t, pfull = b_pfull + 16 * t, pvdone = b_pvdone + 16 * t;
+    const uint32_t sfull = b_sfull + 8 * t, pfull = b_pfull + 16 * t, phalf = b_phalf + 16 * t, pvdone = b_pvdone + 16 * t;
     const uint64_t sc2 = pack_f2(a.scale_log2, a.scale_log2);
     const int G = a.cache.group, used = f.tpt * G;
     uint32_t cnt = 0;                        // steps this tile has been through (barrier phases)
@@ -221,55 +223,42 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
         mbar_wait(sfull, cnt & 1, wc);
         __syncwarp();            // the waits may leave the warp diverged; tcgen05.ld/st are warp-collective
         tc_fence_after();
-        uint32_t sc[64];
+        // Half of the columns at a time: 32 scores a thread (all 64 in registers spill, and with the shared memory that this kernel takes
+        // there is no L1 to spill to: 5300 clk a step instead of CLK at head_dim 128).
         const uint32_t col_s = D == 64 ? col_t + 64 * (cnt & 1) : col_t;
-        XKV_TMEM_LD_64(col_s, sc, 0);
-        XKV_TMEM_LD_64(col_s + 64, sc, 32);
-        tc_wait_ld();
-        tc_fence_before();
-        if (D == 64) mbar_arrive(b_sfree + 8 * t);
-        if (first + kUnit > least) {
-          const int la = lim_a - first - cq2, lb = lim_b - first - cq2;
+        uint32_t sc[32];
+        auto load = [&](int half) {
+          XKV_TMEM_LD_64(col_s + 64 * half, sc, 0);
+          tc_wait_ld();
+          if (first + kUnit > least) {
+            const int la = lim_a - first - 64 * half - cq2, lb = lim_b - first - 64 * half - cq2;
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (8 * (i >> 2) + (i & 1) >= ((i & 2) ? lb : la)) sc[i] = 0xff800000u;           // -inf: exponential 0
-        }
-        float mx0 = -INFINITY, mx1 = -INFINITY;
-#pragma unroll
-        for (int g = 0; g < 16; ++g) {
-          mx0 = max3(mx0, __uint_as_float(sc[4 * g]), __uint_as_float(sc[4 * g + 1]));
-          mx1 = max3(mx1, __uint_as_float(sc[4 * g + 2]), __uint_as_float(sc[4 * g + 3]));
-        }
-#pragma unroll
-        for (int o = 1; o < 4; o <<= 1) {
-          mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
-          mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
-        }
-        mx0 *= a.scale_log2;
-        mx1 *= a.scale_log2;
-        // The reference maximum moves only when the row maximum grew by more than 2^kGrow over it; then the sums and (at the
-        // end of the step, when the registers are free) the accumulator are rescaled.
-        float alpha0 = 1.f, alpha1 = 1.f;
-        const bool grow = mx0 > m0 + kGrow || mx1 > m1 + kGrow;
-        if (grow) {
-          if (mx0 > m0 + kGrow) {
-            alpha0 = exp2f(m0 - mx0);      // 0 on the first tile (-inf)
-            m0 = mx0;
-            l0 = mul_f2(l0, pack_f2(alpha0, alpha0));
+            for (int i = 0; i < 32; ++i)
+              if (8 * (i >> 2) + (i & 1) >= ((i & 2) ? lb : la)) sc[i] = 0xff800000u;           // -inf: exponential 0
           }
-          if (mx1 > m1 + kGrow) {
-            alpha1 = exp2f(m1 - mx1);
-            m1 = mx1;
-            l1 = mul_f2(l1, pack_f2(alpha1, alpha1));
-          }
-        }
-        const float ref0 = m0 == -INFINITY ? 0.f : -m0, ref1 = m1 == -INFINITY ? 0.f : -m1;      // (a row that has seen nothing yet)
-        const uint64_t nm0 = pack_f2(ref0, ref0), nm1 = pack_f2(ref1, ref1);
-        const uint32_t colP = D == 64 ? col_t + 128 * (cnt & 1) : col_t;       // (over scores of these rows only)
-        auto columns = [&](int g0, uint32_t* pk) {
+        };
+        auto tops = [&](float& top0, float& top1) {
 #pragma unroll
           for (int g = 0; g < 8; ++g) {
-            const uint32_t* x = sc + 4 * (g0 + g);
+            top0 = max3(top0, __uint_as_float(sc[4 * g]), __uint_as_float(sc[4 * g + 1]));
+            top1 = max3(top1, __uint_as_float(sc[4 * g + 2]), __uint_as_float(sc[4 * g + 3]));
+          }
+        };
+        auto over_quad = [&](float& top0, float& top1) {       // (and scaled)
+#pragma unroll
+          for (int o = 1; o < 4; o <<= 1) {
+            top0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, o));
+            top1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, o));
+          }
+          top0 *= a.scale_log2;
+          top1 *= a.scale_log2;
+        };
+        auto columns = [&](uint32_t* pk) {
+          const float ref0 = m0 == -INFINITY ? 0.f : -m0, ref1 = m1 == -INFINITY ? 0.f : -m1;      // (a row that sees nothing)
+          const uint64_t nm0 = pack_f2(ref0, ref0), nm1 = pack_f2(ref1, ref1);
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {
+            const uint32_t* x = sc + 4 * g;
             const uint64_t x0 = fma_f2(pack_f2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, nm0);
             const uint64_t x1 = fma_f2(pack_f2(__uint_as_float(x[2]), __uint_as_float(x[3])), sc2, nm1);
             const float e0 = fast_exp2(f2_lo(x0)), e1 = fast_exp2(f2_hi(x0)), e2 = fast_exp2(f2_lo(x1)), e3 = fast_exp2(f2_hi(x1));
@@ -279,18 +268,55 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
             pk[2 * g + 1] = BF16 ? pack_bf2(e2, e3) : pack_h2(e2, e3);
           }
         };
-        {
-          uint32_t pk[16];
-          columns(0, pk); XKV_TMEM_ST_P32(colP, pk);
-          columns(8, pk); XKV_TMEM_ST_P32(colP + 32, pk);
+        // The reference maximum of a row is its maximum over the part's first unit, and moves only when the row's maximum has grown by more
+        // than 2^kGrow over it.  So the exponentials of a later unit need not wait for its maxima: they are computed against the
+        // reference as it is, the maxima beside them, and in the rare case that a row has outgrown its reference, once more.
+        if (jj == 0) {
+          load(0);
+          tops(m0, m1);
+          load(1);
+          tops(m0, m1);
+          over_quad(m0, m1);
         }
-        if (jj > 0 && __any_sync(0xffffffffu, grow)) {
-          // the accumulator is quiescent once the previous step's PV has completed
-          mbar_wait(pvdone + 8 * ((cnt - 1) & 1), ((cnt - 1) >> 1) & 1, wc);
-          __syncwarp();
-          tc_fence_after();
-          rescale_chunk_rows<D>(colO, alpha0, alpha1);
+        const uint32_t colP = D == 64 ? col_t + 128 * (cnt & 1) : col_t;       // (over scores of these rows only)
+        uint32_t pk[16];
+        float top0 = -INFINITY, top1 = -INFINITY;
+        const uint64_t l0_before = l0, l1_before = l1;
+        load(0);
+        tops(top0, top1);
+        columns(pk);
+        load(1);
+        if (jj > 0) {
+          tops(top0, top1);
+          over_quad(top0, top1);
+          if (__any_sync(0xffffffffu, top0 > m0 + kGrow || top1 > m1 + kGrow)) {
+            float alpha0 = 1.f, alpha1 = 1.f;
+            if (top0 > m0 + kGrow) { alpha0 = exp2f(m0 - top0); m0 = top0; }
+            if (top1 > m1 + kGrow) { alpha1 = exp2f(m1 - top1); m1 = top1; }
+            l0 = mul_f2(l0_before, pack_f2(alpha0, alpha0));
+            l1 = mul_f2(l1_before, pack_f2(alpha1, alpha1));
+            load(0);
+            columns(pk);
+            // the accumulator is quiescent once the previous step's PV has completed
+            mbar_wait(pvdone + 8 * ((cnt - 1) & 1), ((cnt - 1) >> 1) & 1, wc);
+            __syncwarp();
+            tc_fence_after();
+            rescale_chunk_rows<D>(colO, alpha0, alpha1);
+            load(1);
+          }
         }
+        if (D == 64) {
+          tc_fence_before();
+          mbar_arrive(b_sfree + 8 * t);
+        }
+        XKV_TMEM_ST_P32(colP, pk);
+        if (D == 128) {          // the first half of P V may begin
+          tc_wait_st();
+          tc_fence_before();
+          mbar_arrive(phalf + 8 * (cnt & 1));
+        }
+        columns(pk);
+        XKV_TMEM_ST_P32(colP + 32, pk);
         tc_wait_st();
         tc_fence_before();
         mbar_arrive(pfull + 8 * (cnt & 1));
@@ -400,24 +426,33 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       const int valid = walk.q.len - (walk.tile_lo + jj) * kUnit;
       const int steps = valid >= kUnit ? 8 : max(1, (valid + 15) / 16);
       mbar_wait(b_vfull + 8 * vb, vph, wc);
-      if (active) {
-        mbar_wait(b_pfull + 16 * t + 8 * (c & 1), (c >> 1) & 1, wc);
-        if (jj == 0 && cq > 0) mbar_wait(b_ofree + 8 * t, (cq - 1) & 1, wc);
-      }
       if (valid < kUnit && (valid & 15) && valid > 0) { mbar_wait(b_vfix + 8 * vb, (fix >> vb) & 1, wc); fix ^= 1u << vb; }
-      __syncwarp();
-      tc_fence_after();
-      if (elect_one()) {
-        if (active) {
-          const uint64_t dv = dv0 + (uint64_t)(vb * (kTile >> 4));
-          const uint32_t d_p = D == 64 ? d_tile + 128 * (c & 1) : d_tile;
+      const uint64_t dv = dv0 + (uint64_t)(vb * (kTile >> 4));
+      const uint32_t d_p = D == 64 ? d_tile + 128 * (c & 1) : d_tile;
+      auto multiply = [&](int from, int to) {
+        __syncwarp();
+        tc_fence_after();
+        if (elect_one()) {
 #pragma unroll
-          for (int ks = 0; ks < 8; ++ks)   // 16 tokens per step: 2048 B of every slab of V, 8 columns of P
+          for (int ks = from; ks < to; ++ks)   // 16 tokens per step: 2048 B of every slab of V, 8 columns of P
             if (ks < steps) mma_ts(d_o, d_p + 8 * ks, dv + (uint64_t)((ks * 2048) >> 4), idesc_pv, (jj > 0 || ks > 0) ? 1u : 0u);
-          tc_commit(b_pvdone + 16 * t + 8 * (c & 1));
+          if (to == 8) tc_commit(b_pvdone + 16 * t + 8 * (c & 1));
         }
-        tc_commit(b_vfree + 8 * vb);
+        __syncwarp();
+      };
+      if (active) {
+        if (D == 128) mbar_wait(b_phalf + 16 * t + 8 * (c & 1), (c >> 1) & 1, wc);
+        else mbar_wait(b_pfull + 16 * t + 8 * (c & 1), (c >> 1) & 1, wc);
+        if (jj == 0 && cq > 0) mbar_wait(b_ofree + 8 * t, (cq - 1) & 1, wc);
+        if (D == 128) {
+          multiply(0, 4);
+          mbar_wait(b_pfull + 16 * t + 8 * (c & 1), (c >> 1) & 1, wc);
+          multiply(4, 8);
+        } else {
+          multiply(0, 8);
+        }
       }
+      if (elect_one()) tc_commit(b_vfree + 8 * vb);
       __syncwarp();
       if (++vb == (uint32_t)kNV) { vb = 0; vph ^= 1; }
     };
