@@ -38,7 +38,7 @@ template <int D> struct Chunk {
   static constexpr int kTile = kSlabs * 16384;
   static constexpr int kNK = D == 64 ? 4 : 2, kNV = D == 64 ? 4 : 2;
   static constexpr int kOffK = 2 * kTile, kOffV = kOffK + kNK * kTile, kOffBar = kOffV + kNV * kTile;
-  static constexpr int kBars = 2 * kNK + 3 * kNV + 2 + 2 + 2 + 2 + 4 + 4 + 2 + 4;
+  static constexpr int kBars = 2 * kNK + 3 * kNV + 2 + 2 + 2 + 2 + 4 + 4 + 2 + 4 + 2;
   static constexpr int kOffPrefix = kOffBar + 512;
   static constexpr size_t kBytes = kOffPrefix + (kMaxSeqs + 1) * 4 + 1024;
   // tensor memory columns
@@ -63,46 +63,64 @@ __device__ __forceinline__ int seen_by(const PagedAttnArgs& a, const Seq& q, int
   return a.full ? q.len : max(0, q.len - q.n_new + min(q.n_new, toks));
 }
 
+// An item counts for some units more than it has: its queries, first scores and results take that long.
+constexpr uint32_t kItemCost = 2;
+
 // The parts of items in a block's piece, one after the other.
 struct ChunkWalk {
-  uint32_t pos, end;
+  uint32_t pos, end;                         // on the line, which has kItemCost + units places per item
   Seq q;
-  int seq, head, pair, tile_lo, nt;          // units [tile_lo, tile_lo + nt) of the item
+  int seq, head, pair, pairs;
+  int tile_lo, nt;                           // units [tile_lo, tile_lo + nt) of the item
   int units;                                 // of the item
-  int ntt[2];                                // of them those of tile 0 and 1
-  uint32_t item_lo;
-  __device__ __forceinline__ bool next(const ChunkArgs& f, const uint32_t* prefix) {
-    if (pos >= end) return false;
-    seq = line_seq(prefix, f.a.seqs.n_seqs, pos);
+  int nt0, nt1;                              // of them those of tile 0 and 1
+  uint32_t item_lo;                          // the item's place on the line
+  __device__ __forceinline__ void start(uint32_t from, uint32_t to) { pos = from; end = to; seq = -1; }
+  __device__ __forceinline__ void open(const ChunkArgs& f) {
     q = seq_at(f.a.cache, f.a.seqs, seq);
-    const uint32_t per = (prefix[seq + 1] - prefix[seq]) / (uint32_t)f.a.cache.n_kv_heads;
-    uint32_t rel = pos - prefix[seq];
-    head = (int)(rel / per);
-    rel -= (uint32_t)head * per;
-    pair = 0;
-    if (f.a.full) {
-      const uint32_t u = (uint32_t)units_of(q.len);
-      pair = (int)(rel / u);
-      rel -= (uint32_t)pair * u;
-      units = (int)u;
-    } else {
-      for (;; ++pair) {
+    pairs = (q.n_new + 2 * f.tpt - 1) / (2 * f.tpt);
+  }
+  __device__ __forceinline__ bool next(const ChunkArgs& f, const uint32_t* prefix) {
+    uint32_t rel = 0;                        // place within the item
+    do {
+      if (pos >= end) return false;
+      if (seq < 0) {                         // where the piece begins
+        seq = line_seq(prefix, f.a.seqs.n_seqs, pos);
+        open(f);
+        const uint32_t per = (prefix[seq + 1] - prefix[seq]) / (uint32_t)f.a.cache.n_kv_heads;
+        rel = pos - prefix[seq];
+        head = (int)(rel / per);
+        rel -= (uint32_t)head * per;
+        for (pair = 0;; ++pair) {
+          units = units_of(seen_by(f.a, q, (pair + 1) * 2 * f.tpt));
+          if (rel < (uint32_t)units + kItemCost) break;
+          rel -= (uint32_t)units + kItemCost;
+        }
+      } else {                               // the next item begins
+        rel = 0;
+        if (++pair == pairs) {
+          pair = 0;
+          if (++head == f.a.cache.n_kv_heads) {
+            head = 0;
+            do ++seq; while (prefix[seq + 1] == pos);
+            open(f);
+          }
+        }
         units = units_of(seen_by(f.a, q, (pair + 1) * 2 * f.tpt));
-        if (rel < (uint32_t)units) break;
-        rel -= (uint32_t)units;
       }
-    }
-    item_lo = pos - rel;
-    tile_lo = (int)rel;
-    nt = (int)min((uint32_t)units - rel, end - pos);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int tok0 = (2 * pair + t) * f.tpt;
-      const int ut = tok0 < q.n_new ? units_of(seen_by(f.a, q, tok0 + f.tpt)) : 0;
-      ntt[t] = max(0, min(nt, ut - tile_lo));
-    }
-    pos += (uint32_t)nt;
+      item_lo = pos - rel;
+      const uint32_t stop = min((uint32_t)units + kItemCost - rel, end - pos);
+      tile_lo = (int)(max(rel, kItemCost) - kItemCost);
+      nt = (int)(max(rel + stop, kItemCost) - kItemCost) - tile_lo;
+      pos += stop;
+    } while (nt == 0);                       // (no more than the cost of an item that begins here)
+    nt0 = part_of(f, 2 * pair);
+    nt1 = part_of(f, 2 * pair + 1);
     return true;
+  }
+  __device__ __forceinline__ int part_of(const ChunkArgs& f, int tile) const {
+    const int ut = tile * f.tpt < q.n_new ? units_of(seen_by(f.a, q, (tile + 1) * f.tpt)) : 0;
+    return max(0, min(nt, ut - tile_lo));
   }
 };
 
@@ -149,6 +167,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
   const uint32_t b_pvdone = b_sfree + 16, b_pfull = b_pvdone + 32, b_ofree = b_pfull + 32;
   const uint32_t b_vfix = b_ofree + 16;       // [kNV], one per stage: a stage is not filled again before both tiles have passed it
   const uint32_t b_phalf = b_vfix + 8 * kNV;  // [2 tiles][2] head_dim 128: P of the unit's first 64 tokens written
+  const uint32_t b_turn = b_phalf + 32;       // [2] head_dim 128: it is this tile's turn at the exponentials
   static_assert(8 * C::kBars <= 512 - 16, "barriers");
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(sgen + C::kOffBar + 496);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sgen + C::kOffBar + 500);
@@ -170,6 +189,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       mbar_init(b_phalf + 16 * t, kRowThreads); mbar_init(b_phalf + 16 * t + 8, kRowThreads);
     }
     for (int i = 0; i < kNV; ++i) mbar_init(b_vfix + 8 * i, 32);
+    for (int t = 0; t < 2; ++t) mbar_init(b_turn + 8 * t, 8);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kSW) {
@@ -181,8 +201,8 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
     const Seq q = seq_at(a.cache, a.seqs, s);
     const int pairs = (q.n_new + 2 * f.tpt - 1) / (2 * f.tpt);
     uint32_t u = 0;
-    if (a.full) u = (uint32_t)pairs * (uint32_t)units_of(q.len);
-    else for (int p = 0; p < pairs; ++p) u += (uint32_t)units_of(seen_by(a, q, (p + 1) * 2 * f.tpt));
+    if (a.full) u = (uint32_t)pairs * ((uint32_t)units_of(q.len) + kItemCost);
+    else for (int p = 0; p < pairs; ++p) u += (uint32_t)units_of(seen_by(a, q, (p + 1) * 2 * f.tpt)) + kItemCost;
     return u * (uint32_t)a.cache.n_kv_heads;
   });
   tc_fence_before();
@@ -191,8 +211,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
   const Cut cut(prefix[a.seqs.n_seqs], gridDim.x);
   ChunkWalk walk;
-  walk.pos = cut.start(blockIdx.x);
-  walk.end = cut.start(blockIdx.x + 1);
+  walk.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1));
 
   if (warp < kSW) {
     // ============== softmax warps, 16 rows of a tile each ==============
@@ -205,9 +224,10 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
     const uint32_t sfull = b_sfull + 8 * t, pfull = b_pfull + 16 * t, phalf = b_phalf + 16 * t, pvdone = b_pvdone + 16 * t;
     const uint64_t sc2 = pack_f2(a.scale_log2, a.scale_log2);
     const int G = a.cache.group, used = f.tpt * G;
+    uint32_t turns = 0;                      // steps at which the tiles took turns so far
     uint32_t cnt = 0;                        // steps this tile has been through (barrier phases)
     for (int part = 0; walk.next(f, prefix); ++part) {
-      const int nt = walk.ntt[t];
+      const int nt = t ? walk.nt1 : walk.nt0;
       const int tok0 = (2 * walk.pair + t) * f.tpt;
       if (tok0 >= walk.q.n_new) continue;       // the pair has no second tile
       const int tok_a = tok0 + r / G, tok_b = tok0 + (r + 8) / G;
@@ -224,7 +244,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
         __syncwarp();            // the waits may leave the warp diverged; tcgen05.ld/st are warp-collective
         tc_fence_after();
         // Half of the columns at a time: 32 scores a thread (all 64 in registers spill, and with the shared memory that this kernel takes
-        // there is no L1 to spill to: 5300 clk a step instead of CLK at head_dim 128).
+        // there is no L1 to spill to: chunks of four prompts 674 us instead of 646, at that time).
         const uint32_t col_s = D == 64 ? col_t + 64 * (cnt & 1) : col_t;
         uint32_t sc[32];
         auto load = [&](int half) {
@@ -282,8 +302,17 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
         uint32_t pk[16];
         float top0 = -INFINITY, top1 = -INFINITY;
         const uint64_t l0_before = l0, l1_before = l1;
+        // head_dim 128: the tiles take turns at the exponentials: while one has the special-function units to itself, the MMAs of the
+        // other run.  (Left alone they fall into step, both at their exponentials and then both at their MMAs: 583 us for the
+        // chunks of four prompts instead of 525.  head_dim 64 has its scores a step ahead and loses 10 % by turns.)
+        const bool both = D == 128 && jj < min(walk.nt0, walk.nt1);
         load(0);
         tops(top0, top1);
+        if (both) {
+          if (t) mbar_wait(b_turn + 8, turns & 1, wc);
+          else if (turns > 0) mbar_wait(b_turn, (turns - 1) & 1, wc);
+          __syncwarp();
+        }
         columns(pk);
         load(1);
         if (jj > 0) {
@@ -316,6 +345,11 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
           mbar_arrive(phalf + 8 * (cnt & 1));
         }
         columns(pk);
+        if (both) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_turn + 8 * (t ^ 1));
+          ++turns;
+        }
         XKV_TMEM_ST_P32(colP + 32, pk);
         tc_wait_st();
         tc_fence_before();
@@ -457,7 +491,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       if (++vb == (uint32_t)kNV) { vb = 0; vph ^= 1; }
     };
     while (walk.next(f, prefix)) {
-      const int nt = t ? walk.ntt[1] : walk.ntt[0];
+      const int nt = t ? walk.nt1 : walk.nt0;
       if (D == 64) {
         // the scores are a whole step ahead of P V
 #pragma unroll 1
@@ -483,7 +517,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
     while (walk.next(f, prefix)) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (walk.ntt[t] == 0) continue;
+        if ((t ? walk.nt1 : walk.nt0) == 0) continue;
         if (cq[t] > 0) mbar_wait<1000>(b_qfree + 8 * t, (cq[t] - 1) & 1, wc);
         __syncwarp();
         if (lane == 0) {
@@ -571,12 +605,11 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       CutItem ci;
       ci.parts = 0;
       ChunkWalk w;
-      w.pos = cut.start(blockIdx.x);
-      w.end = cut.start(blockIdx.x + 1);
+      w.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1));
       for (int part = 0; w.next(f, prefix); ++part) {
         if (w.tile_lo == 0 && w.nt < w.units) {
           ci.row0 = w.q.row0; ci.n_new = w.q.n_new; ci.head = w.head; ci.pair = w.pair;
-          ci.parts = (int)cut.owner(w.item_lo + (uint32_t)w.units - 1) - (int)blockIdx.x + 1;
+          ci.parts = (int)cut.owner(w.item_lo + kItemCost + (uint32_t)w.units - 1) - (int)blockIdx.x + 1;
           ci.slot0 = 2 * blockIdx.x + (part == 0 ? 0 : 1);
         }
       }
@@ -619,13 +652,14 @@ __global__ void __launch_bounds__(kMergeRows * D / 8) chunk_merge_kernel(const _
         const size_t slot = p0 + j == 0 ? (size_t)ci.slot0 : (size_t)2 * (blockIdx.y + p0 + j);
         const size_t prow = (slot * 2 + t) * 128 + r;
         ml[j] = f.s.ml[prow];
-        if (ml[j].x != -INFINITY) {         // (a part without this tile has no accumulators)
-          const float4* po = reinterpret_cast<const float4*>(f.s.o + prow * D + c);
-          x[j] = po[0];
-          y[j] = po[1];
-        }
+        const float4* po = reinterpret_cast<const float4*>(f.s.o + prow * D + c);
+        x[j] = po[0];
+        y[j] = po[1];
       }
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)             // (a part without this tile has no accumulators: whatever was there before)
+      if (ml[j].x == -INFINITY) x[j] = y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
     const float mc = fmaxf(fmaxf(m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x));
     const float ref = mc == -INFINITY ? 0.f : mc;
     const float sc = exp2f(m - ref);
