@@ -55,6 +55,7 @@ struct ChunkArgs {
   CutItem* cuts;          // [blocks]
   int tpt;                // tokens of a tile
   int box_rows;           // slots of a copy: min(page_tokens, 128)
+  int q_toks;             // tokens of a copy of queries: those of a tile, or fewer if no sequence has that many new ones
 };
 
 __device__ __forceinline__ int units_of(int vis) { return max(1, (vis + kUnit - 1) / kUnit); }
@@ -63,19 +64,16 @@ __device__ __forceinline__ int seen_by(const PagedAttnArgs& a, const Seq& q, int
   return a.full ? q.len : max(0, q.len - q.n_new + min(q.n_new, toks));
 }
 
-// An item counts for some units more than it has: its queries, first scores and results take that long.
-constexpr uint32_t kItemCost = 2;
-
 // The parts of items in a block's piece, one after the other.
 struct ChunkWalk {
-  uint32_t pos, end;                         // on the line, which has kItemCost + units places per item
+  uint32_t pos, end, cost;                   // on the line, which has cost + units places per item
   Seq q;
   int seq, head, pair, pairs;
   int tile_lo, nt;                           // units [tile_lo, tile_lo + nt) of the item
   int units;                                 // of the item
   int nt0, nt1;                              // of them those of tile 0 and 1
   uint32_t item_lo;                          // the item's place on the line
-  __device__ __forceinline__ void start(uint32_t from, uint32_t to) { pos = from; end = to; seq = -1; }
+  __device__ __forceinline__ void start(uint32_t from, uint32_t to, uint32_t item_cost) { pos = from; end = to; cost = item_cost; seq = -1; }
   __device__ __forceinline__ void open(const ChunkArgs& f) {
     q = seq_at(f.a.cache, f.a.seqs, seq);
     pairs = (q.n_new + 2 * f.tpt - 1) / (2 * f.tpt);
@@ -93,8 +91,8 @@ struct ChunkWalk {
         rel -= (uint32_t)head * per;
         for (pair = 0;; ++pair) {
           units = units_of(seen_by(f.a, q, (pair + 1) * 2 * f.tpt));
-          if (rel < (uint32_t)units + kItemCost) break;
-          rel -= (uint32_t)units + kItemCost;
+          if (rel < (uint32_t)units + cost) break;
+          rel -= (uint32_t)units + cost;
         }
       } else {                               // the next item begins
         rel = 0;
@@ -109,9 +107,9 @@ struct ChunkWalk {
         units = units_of(seen_by(f.a, q, (pair + 1) * 2 * f.tpt));
       }
       item_lo = pos - rel;
-      const uint32_t stop = min((uint32_t)units + kItemCost - rel, end - pos);
-      tile_lo = (int)(max(rel, kItemCost) - kItemCost);
-      nt = (int)(max(rel + stop, kItemCost) - kItemCost) - tile_lo;
+      const uint32_t stop = min((uint32_t)units + cost - rel, end - pos);
+      tile_lo = (int)(max(rel, cost) - cost);
+      nt = (int)(max(rel + stop, cost) - cost) - tile_lo;
       pos += stop;
     } while (nt == 0);                       // (no more than the cost of an item that begins here)
     nt0 = part_of(f, 2 * pair);
@@ -173,7 +171,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sgen + C::kOffBar + 500);
   const WaitCtx wc{sbase + C::kOffBar + 500};
   uint32_t* prefix = reinterpret_cast<uint32_t*>(sgen + C::kOffPrefix);
-  __shared__ uint32_t s_warp[kThreads / 32];
+  __shared__ uint2 s_warp[kThreads / 32];
 
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -197,13 +195,15 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   grid_dependency_wait();
-  line_prefix<kThreads>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {
+  const uint32_t cost = line_prefix<kThreads>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {
     const Seq q = seq_at(a.cache, a.seqs, s);
     const int pairs = (q.n_new + 2 * f.tpt - 1) / (2 * f.tpt);
-    uint32_t u = 0;
-    if (a.full) u = (uint32_t)pairs * ((uint32_t)units_of(q.len) + kItemCost);
-    else for (int p = 0; p < pairs; ++p) u += (uint32_t)units_of(seen_by(a, q, (p + 1) * 2 * f.tpt)) + kItemCost;
-    return u * (uint32_t)a.cache.n_kv_heads;
+    Work w = {(uint32_t)pairs, 0u};
+    if (a.full) w.units = (uint32_t)pairs * (uint32_t)units_of(q.len);
+    else for (int p = 0; p < pairs; ++p) w.units += (uint32_t)units_of(seen_by(a, q, (p + 1) * 2 * f.tpt));
+    w.items *= (uint32_t)a.cache.n_kv_heads;
+    w.units *= (uint32_t)a.cache.n_kv_heads;
+    return w;
   });
   tc_fence_before();
   __syncthreads();
@@ -211,7 +211,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
   const Cut cut(prefix[a.seqs.n_seqs], gridDim.x);
   ChunkWalk walk;
-  walk.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1));
+  walk.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1), cost);
 
   if (warp < kSW) {
     // ============== softmax warps, 16 rows of a tile each ==============
@@ -521,7 +521,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
         if (cq[t] > 0) mbar_wait<1000>(b_qfree + 8 * t, (cq[t] - 1) & 1, wc);
         __syncwarp();
         if (lane == 0) {
-          mbar_expect_tx(b_qfull + 8 * t, (uint32_t)(kSlabs * 128 * f.tpt * a.cache.group));
+          mbar_expect_tx(b_qfull + 8 * t, (uint32_t)(kSlabs * 128 * f.q_toks * a.cache.group));
 #pragma unroll
           for (int c = 0; c < kSlabs; ++c)
             tma_3d(sQ + t * kTile + c * 16384, &q_map, 64 * c, walk.head * a.cache.group, walk.q.row0 + (2 * walk.pair + t) * f.tpt, b_qfull + 8 * t);
@@ -605,11 +605,11 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       CutItem ci;
       ci.parts = 0;
       ChunkWalk w;
-      w.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1));
+      w.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1), cost);
       for (int part = 0; w.next(f, prefix); ++part) {
         if (w.tile_lo == 0 && w.nt < w.units) {
           ci.row0 = w.q.row0; ci.n_new = w.q.n_new; ci.head = w.head; ci.pair = w.pair;
-          ci.parts = (int)cut.owner(w.item_lo + kItemCost + (uint32_t)w.units - 1) - (int)blockIdx.x + 1;
+          ci.parts = (int)cut.owner(w.item_lo + cost + (uint32_t)w.units - 1) - (int)blockIdx.x + 1;
           ci.slot0 = 2 * blockIdx.x + (part == 0 ? 0 : 1);
         }
       }
@@ -708,8 +708,9 @@ cudaError_t launch_attn_chunk(const PagedAttnArgs& a, const PoolMaps& maps, cons
   f.cuts = reinterpret_cast<CutItem*>(cuts);
   f.tpt = 128 / a.cache.group;
   f.box_rows = min(1 << a.cache.page_shift, 128);
+  f.q_toks = min(f.tpt, a.seqs.max_new);
   CUtensorMap q_map;
-  cudaError_t e = make_token_map(a.q, a.q_ts, a.q_hs, a.seqs.n_tokens, a.cache.n_heads, head_dim, dtype, a.cache.group, f.tpt, &q_map);
+  cudaError_t e = make_token_map(a.q, a.q_ts, a.q_hs, a.seqs.n_tokens, a.cache.n_heads, head_dim, dtype, a.cache.group, f.q_toks, &q_map);
   if (e != cudaSuccess) return e;
   const int grid = sm_count;
   void* p0[3] = {(void*)&f, (void*)&maps, (void*)&q_map};

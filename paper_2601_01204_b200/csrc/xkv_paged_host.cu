@@ -77,7 +77,7 @@ Layout make_layout(const xkv_paged_params* p, int sms) {
 bool work_ok(const xkv_paged* c, const xkv_paged_batch* b) {
   const int64_t units = (int64_t)b->table_width * c->p.page_tokens / 128 + 2;
   const int64_t tiles = (int64_t)b->max_new * c->view.group / (kChunkRows / 2) + 2;
-  return (double)b->n_seqs * c->p.n_kv_heads * (double)units * (double)tiles < 4294967296.0;
+  return (double)b->n_seqs * c->p.n_kv_heads * (double)(units + 2) * (double)tiles < 4294967296.0;
 }
 
 bool batch_ok(const xkv_paged* c, const xkv_paged_batch* b, bool tokens) {

@@ -21,38 +21,52 @@ struct Cut {
   }
 };
 
-// prefix[s] = units before sequence s, prefix[n_seqs] = all of them; `units` gives a sequence's.  All THREADS threads of the block
-// (at least 32 * 32 / 8, a multiple of 32) call it; it ends with a barrier.
+// What is done once per item (queries, first scores, merging, results) takes as long as some units.  Where a block's piece is long
+// an item therefore has kItemCost more places on the line than it has units, so that blocks with many short items have fewer
+// units; where pieces are a few units only, those count.
+constexpr uint32_t kItemCost = 2, kLongPiece = 8;
+
+// prefix[s] = places on the line before sequence s, prefix[n_seqs] = all of them; `work` gives a sequence's items and units.  All THREADS
+// threads of the block (a multiple of 32) call it; it ends with a barrier.  Returns the places that an item has more than units.
+struct Work { uint32_t items, units; };
 template <int THREADS, typename F>
-__device__ __forceinline__ void line_prefix(int n_seqs, uint32_t* prefix, uint32_t* s_warp, F units) {
+__device__ __forceinline__ uint32_t line_prefix(int n_seqs, uint32_t* prefix, uint2* s_warp, F work) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (n_seqs + THREADS - 1) / THREADS;
-  uint32_t sum = 0;
+  uint2 sum = make_uint2(0, 0);
   for (int i = 0; i < per; ++i) {
     const int s = tid * per + i;
-    const uint32_t u = s < n_seqs ? units(s) : 0u;
-    if (s < n_seqs) prefix[s] = sum;               // (of this thread's own so far)
-    sum += u;
+    if (s >= n_seqs) break;
+    const Work w = work(s);
+    sum.x += w.items; sum.y += w.units;
   }
-  uint32_t inc = sum;
+  uint2 inc = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += y;
+    const uint32_t x = __shfl_up_sync(0xffffffffu, inc.x, o), y = __shfl_up_sync(0xffffffffu, inc.y, o);
+    if (lane >= o) { inc.x += x; inc.y += y; }
   }
   if (lane == 31) s_warp[warp] = inc;
   __syncthreads();
-  uint32_t before = inc - sum;
-  for (int w = 0; w < warp; ++w) before += s_warp[w];
+  uint2 before = make_uint2(inc.x - sum.x, inc.y - sum.y), all = make_uint2(0, 0);
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w < warp) { before.x += s_warp[w].x; before.y += s_warp[w].y; }
+    all.x += s_warp[w].x; all.y += s_warp[w].y;
+  }
+  const uint32_t cost = all.y >= kLongPiece * gridDim.x ? kItemCost : 0;
   for (int i = 0; i < per; ++i) {
     const int s = tid * per + i;
-    if (s < n_seqs) prefix[s] += before;
+    if (s >= n_seqs) break;
+    prefix[s] = before.y + cost * before.x;
+    const Work w = work(s);
+    before.x += w.items; before.y += w.units;
   }
-  if (tid == THREADS - 1) prefix[n_seqs] = before + sum;
+  if (tid == 0) prefix[n_seqs] = all.y + cost * all.x;
   __syncthreads();
+  return cost;
 }
 
-// The sequence that a unit belongs to: the last s with prefix[s] <= unit (sequences without units are skipped).
+// The sequence that a place belongs to: the last s with prefix[s] <= place (sequences without work are skipped).
 __device__ __forceinline__ int line_seq(const uint32_t* prefix, int n_seqs, uint32_t unit) {
   int lo = 0, hi = n_seqs;
   while (hi - lo > 1) {

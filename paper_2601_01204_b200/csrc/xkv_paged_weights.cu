@@ -46,6 +46,7 @@ template <int D> struct Weigh {
 struct WeighArgs {
   PagedWeightArgs a;
   int tpt, box_rows;
+  int q_toks;              // tokens of a copy of queries: those of a tile, or fewer if no sequence has that many new ones
 };
 
 // Items of the block: every gridDim.x-th of the line.
@@ -126,7 +127,7 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
   float* s_sum = reinterpret_cast<float*>(sgen + C::kOffSum);        // [kSums][2][128]
   Seq* seqs = reinterpret_cast<Seq*>(sgen + C::kOffSeq);
   uint32_t* prefix = reinterpret_cast<uint32_t*>(sgen + C::kOffPrefix);
-  __shared__ uint32_t s_warp[kThreads / 32];
+  __shared__ uint2 s_warp[kThreads / 32];
 
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -144,10 +145,10 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   grid_dependency_wait();
-  line_prefix<kThreads>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {
+  line_prefix<kThreads>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {       // (items alone count here: none is cut)
     const Seq q = seq_at(a.cache, a.seqs, s);
     seqs[s] = q;
-    return q.n_new == 0 ? 0u : (uint32_t)a.cache.n_kv_heads * (uint32_t)((q.len + 2 * kUnit - 1) / (2 * kUnit));
+    return Work{0u, q.n_new == 0 ? 0u : (uint32_t)a.cache.n_kv_heads * (uint32_t)((q.len + 2 * kUnit - 1) / (2 * kUnit))};
   });
   tc_fence_before();
   __syncthreads();
@@ -318,13 +319,12 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
       mbar_wait<500>(b_kfree + 8 * ks, ((g / kNK) & 1) ^ 1, wc);
       __syncwarp();
       if (lane == 0) mbar_expect_tx(b_kfull + 8 * ks, (uint32_t)(boxes * f.box_rows * 128 * kSlabs));
-      for (int i = 0; i < boxes; ++i) {
+      {
+        const int i = lane / kSlabs, c = lane % kSlabs;         // (a copy per lane)
         const int page = __shfl_sync(0xffffffffu, now, i);
-        if (lane == 0)
-#pragma unroll
-          for (int c = 0; c < kSlabs; ++c)
-            tma_4d(sK + (2 * ks + (i * f.box_rows) / kUnit) * kTile + c * 16384 + ((i * f.box_rows) & (kUnit - 1)) * 128, &maps.k, 64 * c,
-                   (w.first + i * f.box_rows) & page_mask, w.head, page, b_kfull + 8 * ks);
+        if (i < boxes)
+          tma_4d(sK + (2 * ks + (i * f.box_rows) / kUnit) * kTile + c * 16384 + ((i * f.box_rows) & (kUnit - 1)) * 128, &maps.k, 64 * c,
+                 (w.first + i * f.box_rows) & page_mask, w.head, page, b_kfull + 8 * ks);
       }
       ++g;
       for (int j = 0; j < w.tiles; ++j, ++gq) {
@@ -332,7 +332,7 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
         mbar_wait(b_qfree + 8 * qs, ((gq / kNQ) & 1) ^ 1, wc);
         __syncwarp();
         if (lane == 0) {
-          mbar_expect_tx(b_qfull + 8 * qs, (uint32_t)(kSlabs * 128 * f.tpt * G));
+          mbar_expect_tx(b_qfull + 8 * qs, (uint32_t)(kSlabs * 128 * f.q_toks * G));
 #pragma unroll
           for (int c = 0; c < kSlabs; ++c)
             tma_3d(sQ + qs * kTile + c * 16384, &q_map, 64 * c, w.head * G, w.row0 + (w.tile0 + j) * f.tpt, b_qfull + 8 * qs);
@@ -432,8 +432,9 @@ cudaError_t launch_paged_weights(const PagedWeightArgs& a, const PoolMaps& maps,
   f.a = a;
   f.tpt = 128 / a.cache.group;
   f.box_rows = min(1 << a.cache.page_shift, 128);
+  f.q_toks = min(f.tpt, a.seqs.max_new);
   CUtensorMap q_map;
-  cudaError_t e = make_token_map(a.q, a.q_ts, a.q_hs, a.seqs.n_tokens, a.cache.n_heads, head_dim, dtype, a.cache.group, f.tpt, &q_map);
+  cudaError_t e = make_token_map(a.q, a.q_ts, a.q_hs, a.seqs.n_tokens, a.cache.n_heads, head_dim, dtype, a.cache.group, f.q_toks, &q_map);
   if (e != cudaSuccess) return e;
   const bool bf16 = dtype == XKV_BF16;
   const int64_t most = (int64_t)a.seqs.n_seqs * a.cache.n_kv_heads * ((((int64_t)a.seqs.table_width << a.cache.page_shift) + 2 * kUnit - 1) / (2 * kUnit));
