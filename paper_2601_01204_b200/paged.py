@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 from dataclasses import dataclass, field
 
-from .xkv import XKV_E_INVALID, XkvError, _check, _i32, _i64, _sz, _vp, lib
+from .xkv import XKV_E_INVALID, XkvError, _i32, _i64, _sz, _vp, lib
 
 BF16, FP16 = 0, 1
 MASK_CAUSAL, MASK_FULL = 0, 1
@@ -62,60 +62,61 @@ lib.xkv_paged_poll_status.restype = C.c_int
 lib.xkv_paged_poll_status.argtypes = [_vp, _vp]
 
 
+def _refuse(where: str, what: str) -> None:
+    raise XkvError(XKV_E_INVALID, f"{where}: {what}")
+
+
 def _require(ok: bool, where: str, what: str) -> None:
     if not ok:
-        raise XkvError(XKV_E_INVALID, f"{where}: {what}")
+        _refuse(where, what)
 
 
-_torch = None
+# torch, its 16-bit types, and its queries for the current device and its stream (the public ones build an object at each call,
+# which takes as long as a launch)
+_torch = _bf16 = _fp16 = _int32 = _fp32 = _device_now = _stream_of = None
 
 
 def _t():
-    global _torch
+    global _torch, _bf16, _fp16, _int32, _fp32, _device_now, _stream_of
     if _torch is None:
         import torch
+        _bf16, _fp16, _int32, _fp32 = torch.bfloat16, torch.float16, torch.int32, torch.float32
+        _device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda device: torch.cuda.current_stream(device).cuda_stream)
         _torch = torch
     return _torch
 
 
-def _dtype_code(t, where: str) -> int:
-    torch = _t()
-    _require(t.dtype in (torch.bfloat16, torch.float16), where, "tensors are bf16 or fp16")
-    return BF16 if t.dtype == torch.bfloat16 else FP16
-
-
-def _rows(t, where: str, name: str, device: int, dtype, heads: int, n: int, d: int) -> tuple[int, int, int]:
+def _rows(t, where: str, name: str, device: int, dtype, shape: tuple) -> tuple[int, int, int]:
     """(pointer, tok_stride, head_stride) of a token tensor, a [heads][n][d] view with contiguous channels.
     (The stride of a dimension with one entry is never used; torch may give it any value.)"""
-    _require(t.shape == (heads, n, d), where, f"{name} is [{heads}][{n}][{d}], not {list(t.shape)}")
-    _require(t.dtype == dtype and t.get_device() == device, where, f"{name} has another type or device")
+    if t.shape != shape:
+        _refuse(where, f"{name} is {list(shape)}, not {list(t.shape)}")
+    if t.dtype != dtype or t.get_device() != device:
+        _refuse(where, f"{name} has another type or device")
     hs, ts, cs = t.stride()
-    _require(cs == 1, where, f"the channels of {name} are not contiguous")
+    if cs != 1:
+        _refuse(where, f"the channels of {name} are not contiguous")
+    heads, n, d = shape
     return t.data_ptr(), (ts if n > 1 else d), (hs if heads > 1 else d)
 
 
 def _ints(t, where: str, name: str, device: int, shape: tuple) -> int:
-    _require(t.dtype == _t().int32 and t.shape == shape and t.is_contiguous() and t.get_device() == device, where,
-             f"{name} is a contiguous int32 tensor of shape {list(shape)} on the same device")
+    if t.dtype != _int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        _refuse(where, f"{name} is a contiguous int32 tensor of shape {list(shape)} on the same device")
     return t.data_ptr()
 
 
-class _On:
-    """The device's current stream, with that device current for the call."""
-
-    def __init__(self, device: int):
-        torch = _t()
-        self.stream = torch.cuda.current_stream(device).cuda_stream
-        self.guard = None if torch.cuda.current_device() == device else torch.cuda.device(device)
-
-    def __enter__(self) -> int:
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *e) -> None:
-        if self.guard is not None:
-            self.guard.__exit__(*e)
+def _call(device: int, fn, where: str, *args) -> None:
+    """fn(*args, the device's current stream), with that device current."""
+    if _device_now() == device:
+        status = fn(*args, _stream_of(device))
+    else:
+        with _torch.cuda.device(device):
+            status = fn(*args, _stream_of(device))
+    if status:
+        raise XkvError(status, where)
 
 
 @dataclass(frozen=True)
@@ -131,18 +132,21 @@ class RotaryParams:
     beta_slow: float = 1.0
     magnitude: float = 1.0
     struct: xkv_rotary_params = field(init=False, repr=False, compare=False)
+    ref: object = field(init=False, repr=False, compare=False)
 
     def __post_init__(self):
         object.__setattr__(self, "struct", xkv_rotary_params(
             self.rotary_dim, self.n_axes, int(self.interleaved), self.original_tokens, self.base, self.factor,
             self.beta_fast, self.beta_slow, self.magnitude))
+        object.__setattr__(self, "ref", C.byref(self.struct))
 
 
 def _positions(positions, where: str, device: int, n_axes: int, n: int) -> tuple[int, int]:
     if positions.dim() == 1:
         positions = positions[None]
-    _require(positions.dtype == _t().int32 and positions.get_device() == device and positions.shape == (n_axes, n) and
-             (n <= 1 or positions.stride(1) == 1), where, f"positions is int32 [{n_axes}][{n}] on the same device")
+    if positions.dtype != _int32 or positions.get_device() != device or positions.shape != (n_axes, n) or \
+            (n > 1 and positions.stride(1) != 1):
+        _refuse(where, f"positions is int32 [{n_axes}][{n}] on the same device")
     # (one row, or a stride that torch chose for a dimension with one entry)
     return positions.data_ptr(), (positions.stride(0) if n_axes > 1 else n)
 
@@ -150,27 +154,28 @@ def _positions(positions, where: str, device: int, n_axes: int, n: int) -> tuple
 def xkv_rotary(params: RotaryParams, positions, q, k=None, q_out=None, k_out=None, inverse: bool = False):
     """q and k ([heads][n][d] views) turned by their tokens' positions (int32 [n] or [n_axes][n]).
     Returns (q_out, k_out), new tensors unless given; an output may be its input."""
-    torch = _t()
+    torch = _torch or _t()
     where = "xkv_rotary"
-    _require(q.dim() == 3 and q.is_cuda, where, "q is a [heads][n][d] CUDA tensor")
-    device, (H, n, d) = q.get_device(), q.shape
-    code = _dtype_code(q, where)
+    if q.dim() != 3 or not q.is_cuda:
+        _refuse(where, "q is a [heads][n][d] CUDA tensor")
+    device, shape, dtype = q.get_device(), q.shape, q.dtype
+    if dtype != _bf16 and dtype != _fp16:
+        _refuse(where, "tensors are bf16 or fp16")
+    H, n, d = shape
     if q_out is None:
         q_out = torch.empty_like(q)
-    pq, qt, qh = _rows(q, where, "q", device, q.dtype, H, n, d)
-    po, ot, oh = _rows(q_out, where, "q_out", device, q.dtype, H, n, d)
+    pq, qt, qh = _rows(q, where, "q", device, dtype, shape)
+    po, ot, oh = _rows(q_out, where, "q_out", device, dtype, shape)
     pk = pko = kt = kh = kot = koh = K = 0
     if k is not None:
-        _require(k.dim() == 3, where, "k is a [heads][n][d] tensor")
         K = k.shape[0]
         if k_out is None:
             k_out = torch.empty_like(k)
-        pk, kt, kh = _rows(k, where, "k", device, q.dtype, K, n, d)
-        pko, kot, koh = _rows(k_out, where, "k_out", device, q.dtype, K, n, d)
+        pk, kt, kh = _rows(k, where, "k", device, dtype, (K, n, d))
+        pko, kot, koh = _rows(k_out, where, "k_out", device, dtype, (K, n, d))
     pp, ps = _positions(positions, where, device, params.n_axes, n)
-    with _On(device) as stream:
-        _check(lib.xkv_rotary(C.byref(params.struct), code, d, pp, ps, n, pq, po, H, qt, qh, ot, oh,
-                              pk, pko, K, kt, kh, kot, koh, 1 if inverse else 0, stream), where)
+    _call(device, lib.xkv_rotary, where, params.ref, BF16 if dtype == _bf16 else FP16, d, pp, ps, n, pq, po, H, qt, qh, ot, oh,
+          pk, pko, K, kt, kh, kot, koh, 1 if inverse else 0)
     return q_out, k_out
 
 
@@ -192,6 +197,7 @@ class PagedBatch:
 
     def __init__(self, q_start, lens, table, n_tokens: int, max_new: int):
         where = "PagedBatch"
+        _t()
         _require(lens.dim() == 1 and table.dim() == 2 and lens.is_cuda, where, "lens is [n_seqs], table [n_seqs][width], on a GPU")
         self.device, n = lens.get_device(), lens.shape[0]
         self.n_seqs, self.n_tokens = n, n_tokens
@@ -232,10 +238,9 @@ class PagedCache:
         sms = torch.cuda.get_device_properties(self.device).multi_processor_count
         nbytes = int(lib.xkv_paged_workspace_bytes(C.byref(c), sms))
         self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=k_pages.device)
-        with _On(self.device) as stream:
-            _check(lib.xkv_paged_create(C.byref(c), k_pages.data_ptr(), v_pages.data_ptr(),
-                                        weights.data_ptr() if weights is not None else None, self.workspace.data_ptr(),
-                                        nbytes, stream, C.byref(self.handle)), where)
+        _call(self.device, lambda stream: lib.xkv_paged_create(
+            C.byref(c), k_pages.data_ptr(), v_pages.data_ptr(), weights.data_ptr() if weights is not None else None,
+            self.workspace.data_ptr(), nbytes, stream, C.byref(self.handle)), where)
         self.scale = p.head_dim ** -0.5
 
     def close(self) -> None:
@@ -249,30 +254,34 @@ class PagedCache:
         except Exception:
             pass
 
-    def _tokens(self, t, where: str, name: str, batch: PagedBatch, heads: int) -> tuple[int, int, int]:
-        return _rows(t, where, name, self.device, self.dtype, heads, batch.n_tokens, self.p.head_dim)
+    def _shape(self, where: str, batch: PagedBatch, heads: int) -> tuple:
+        if batch.device != self.device:
+            _refuse(where, "the batch is on another device")
+        return heads, batch.n_tokens, self.p.head_dim
 
     # ---- the C calls, same names ------------------------------------------
     def kv_paged_append(self, batch: PagedBatch, k, v, q=None, q_out=None, rotary: RotaryParams | None = None, positions=None):
         """New tokens' k (turned by rotary and positions, if given) and v to their slots; q turned into q_out,
         a new tensor unless given.  Returns q_out."""
         where = "kv_paged_append"
-        p = self.p
-        _require(batch.device == self.device, where, "the batch is on another device")
-        pk, kt, kh = self._tokens(k, where, "k", batch, p.n_kv_heads)
-        pv, vt, vh = self._tokens(v, where, "v", batch, p.n_kv_heads)
+        device, dtype = self.device, self.dtype
+        shape = self._shape(where, batch, self.p.n_kv_heads)
+        pk, kt, kh = _rows(k, where, "k", device, dtype, shape)
+        pv, vt, vh = _rows(v, where, "v", device, dtype, shape)
         pq = po = qt = qh = ot = oh = pp = ps = 0
         if q is not None:
-            pq, qt, qh = self._tokens(q, where, "q", batch, p.n_heads)
+            shape = (self.p.n_heads, batch.n_tokens, self.p.head_dim)
+            pq, qt, qh = _rows(q, where, "q", device, dtype, shape)
             if q_out is None:
-                q_out = _t().empty_like(q)
-            po, ot, oh = self._tokens(q_out, where, "q_out", batch, p.n_heads)
+                q_out = _torch.empty_like(q)
+            po, ot, oh = _rows(q_out, where, "q_out", device, dtype, shape)
+        ref = None
         if rotary is not None:
-            _require(positions is not None, where, "rotary needs positions")
-            pp, ps = _positions(positions, where, self.device, rotary.n_axes, batch.n_tokens)
-        with _On(self.device) as stream:
-            _check(lib.kv_paged_append(self.handle, batch.ref, pk, kt, kh, pv, vt, vh, pq, qt, qh, po, ot, oh,
-                                       C.byref(rotary.struct) if rotary is not None else None, pp, ps, stream), where)
+            if positions is None:
+                _refuse(where, "rotary needs positions")
+            pp, ps = _positions(positions, where, device, rotary.n_axes, batch.n_tokens)
+            ref = rotary.ref
+        _call(device, lib.kv_paged_append, where, self.handle, batch.ref, pk, kt, kh, pv, vt, vh, pq, qt, qh, po, ot, oh, ref, pp, ps)
         return q_out
 
     def attn_paged_causal(self, batch: PagedBatch, q, out=None, lse=None, scale: float | None = None, mask: int = MASK_CAUSAL,
@@ -280,51 +289,47 @@ class PagedCache:
         """Attention of the new tokens over what their sequences hold; out is a new tensor unless given, lse (fp32
         [n_heads][n_tokens], contiguous) is filled if given.  Returns out."""
         where = "attn_paged_causal"
-        H = self.p.n_heads
-        _require(batch.device == self.device, where, "the batch is on another device")
-        pq, qt, qh = self._tokens(q, where, "q", batch, H)
+        shape = self._shape(where, batch, self.p.n_heads)
+        pq, qt, qh = _rows(q, where, "q", self.device, self.dtype, shape)
         if out is None:
-            out = _t().zeros_like(q)        # rows that belong to nobody are not written
-        po, ot, oh = self._tokens(out, where, "out", batch, H)
-        pl = 0 if lse is None else self._lse(lse, where, batch)
-        with _On(self.device) as stream:
-            _check(lib.attn_paged_causal(self.handle, batch.ref, pq, qt, qh, po, ot, oh, pl,
-                                         self.scale if scale is None else scale, mask, impl, stream), where)
+            out = _torch.zeros_like(q)        # rows that belong to nobody are not written
+        po, ot, oh = _rows(out, where, "out", self.device, self.dtype, shape)
+        pl = 0 if lse is None else self._lse(lse, where, shape)
+        _call(self.device, lib.attn_paged_causal, where, self.handle, batch.ref, pq, qt, qh, po, ot, oh, pl,
+              self.scale if scale is None else scale, mask, impl)
         return out
 
-    def _lse(self, lse, where: str, batch: PagedBatch) -> int:
-        _require(lse.dtype == _t().float32 and lse.shape == (self.p.n_heads, batch.n_tokens) and lse.is_contiguous() and
-                 lse.get_device() == self.device, where, "lse is contiguous fp32 [n_heads][n_tokens]")
+    def _lse(self, lse, where: str, shape: tuple) -> int:
+        if lse.dtype != _fp32 or lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != self.device:
+            _refuse(where, "lse is contiguous fp32 [n_heads][n_tokens]")
         return lse.data_ptr()
 
     def kv_paged_weights(self, batch: PagedBatch, q, lse, scale: float | None = None, decay: float = 1.0, mask: int = MASK_CAUSAL) -> None:
         """weights = decay * weights + what the new tokens' softmax gave every cached token (q, lse, scale and mask as
         in attn_paged_causal)."""
         where = "kv_paged_weights"
-        _require(batch.device == self.device, where, "the batch is on another device")
-        pq, qt, qh = self._tokens(q, where, "q", batch, self.p.n_heads)
-        with _On(self.device) as stream:
-            _check(lib.kv_paged_weights(self.handle, batch.ref, pq, qt, qh, self._lse(lse, where, batch),
-                                        self.scale if scale is None else scale, decay, mask, stream), where)
+        shape = self._shape(where, batch, self.p.n_heads)
+        pq, qt, qh = _rows(q, where, "q", self.device, self.dtype, shape)
+        _call(self.device, lib.kv_paged_weights, where, self.handle, batch.ref, pq, qt, qh, self._lse(lse, where, shape),
+              self.scale if scale is None else scale, decay, mask)
 
     def kv_paged_evict(self, batch: PagedBatch, dst_table, keep: int, n_first: int = 0, n_recent: int = 0, kept=None, lens_out=None):
         """Every sequence down to `keep` tokens, moved to the pages of dst_table.  Returns (kept int32
         [n_seqs][n_kv_heads][keep], lens_out int32 [n_seqs]), new tensors unless given."""
-        torch = _t()
         where = "kv_paged_evict"
-        _require(batch.device == self.device and dst_table.dim() == 2, where, "dst_table is [n_seqs][width], the batch on the same device")
-        n = batch.n_seqs
+        device, n = self.device, batch.n_seqs
+        if batch.device != device or dst_table.dim() != 2:
+            _refuse(where, "dst_table is [n_seqs][width], the batch on the same device")
         if kept is None:
-            kept = torch.empty(n, self.p.n_kv_heads, max(keep, 0), dtype=torch.int32, device=dst_table.device)
+            kept = _torch.empty(n, self.p.n_kv_heads, max(keep, 0), dtype=_int32, device=dst_table.device)
         if lens_out is None:
-            lens_out = torch.empty(n, dtype=torch.int32, device=dst_table.device)
-        pd = _ints(dst_table, where, "dst_table", self.device, (n, dst_table.shape[1]))
-        pk = _ints(kept, where, "kept", self.device, (n, self.p.n_kv_heads, max(keep, 0)))
-        pl = _ints(lens_out, where, "lens_out", self.device, (n,))
-        with _On(self.device) as stream:
-            _check(lib.kv_paged_evict(self.handle, batch.ref, pd, dst_table.shape[1], keep, n_first, n_recent, pk, pl, stream), where)
+            lens_out = _torch.empty(n, dtype=_int32, device=dst_table.device)
+        width = dst_table.shape[1]
+        _call(device, lib.kv_paged_evict, where, self.handle, batch.ref, _ints(dst_table, where, "dst_table", device, (n, width)), width,
+              keep, n_first, n_recent, _ints(kept, where, "kept", device, (n, self.p.n_kv_heads, max(keep, 0))),
+              _ints(lens_out, where, "lens_out", device, (n,)))
         return kept, lens_out
 
     def xkv_paged_poll_status(self) -> int:
-        with _On(self.device) as stream:
-            return int(lib.xkv_paged_poll_status(self.handle, stream))
+        with _torch.cuda.device(self.device):
+            return int(lib.xkv_paged_poll_status(self.handle, _stream_of(self.device)))
