@@ -71,26 +71,42 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
   for (int i = tid; i < lo; i += kSelThreads) kept[i] = i;
   for (int i = tid; i < a.n_recent; i += kSelThreads) kept[lo + want + i] = len - a.n_recent + i;
   if (want == 0) return;
-  auto fetch = [&](int j) {                           // key of middle token j
-    const int page = page_at(a.cache, a.seqs.table, a.seqs.table_width, s, lo + j);
-    return page < 0 ? 0u : order_key(a.cache.weights[weight_offset(a.cache, page, h, lo + j)]);
+  const int32_t* table = a.seqs.table + (int64_t)s * a.seqs.table_width;
+  const int shift = a.cache.page_shift;
+  auto key_on = [&](int page, int j) {                // key of middle token j on that page
+    if ((unsigned)page < (unsigned)a.cache.n_pages) return order_key(a.cache.weights[weight_offset(a.cache, page, h, lo + j)]);
+    paged_report(a.cache.status, (int)XKV_E_INVALID);
+    return 0u;
   };
   const int in_smem = min(n, held);
-  for (int j = tid; j < in_smem; j += kSelThreads) s_key[j] = fetch(j);
-  auto key = [&](int j) { return j < in_smem ? s_key[j] : fetch(j); };
+  constexpr int kAhead = 8;                           // tokens of a thread whose pages, and then weights, are asked for at once
+  for (int j0 = tid; j0 < in_smem; j0 += kAhead * kSelThreads) {
+    int page[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + u * kSelThreads;
+      page[u] = j < in_smem ? table[(lo + j) >> shift] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + u * kSelThreads;
+      if (j < in_smem) s_key[j] = key_on(page[u], j);
+    }
+  }
+  auto key = [&](int j) { return j < in_smem ? s_key[j] : key_on(table[(lo + j) >> shift], j); };
   // three digits of 11, 11 and 10 bits from the top: the want-th largest key
   uint32_t prefix = 0;
   int left = want;                                    // rank, from the top, among the keys that match the prefix
 #pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const int digits = pass == 2 ? 1024 : 2048;
     const uint32_t above = pass == 0 ? 0u : pass == 1 ? 0xFFE00000u : 0xFFFFFC00u;
     for (int i = tid; i < 2048; i += kSelThreads) s_hist[i] = 0;
     __syncthreads();
     for (int j = tid; j < n; j += kSelThreads) {
       const uint32_t k = key(j);
-      if ((k & above) == prefix) atomicAdd(&s_hist[(k >> shift) & (digits - 1)], 1u);
+      if ((k & above) == prefix) atomicAdd(&s_hist[(k >> low) & (digits - 1)], 1u);
     }
     __syncthreads();
     // thread t owns digits 2t and 2t + 1 counted from the top
@@ -104,12 +120,13 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
       s_found[1] = (uint32_t)left - before - (first ? 0u : c0);
     }
     __syncthreads();
-    prefix |= s_found[0] << shift;
+    prefix |= s_found[0] << low;
     left = (int)s_found[1];
     __syncthreads();
   }
-  // kept: every key above `prefix`, and the first `left` that equal it.  A thread owns a run of tokens.
-  const int run = (n + kSelThreads - 1) / kSelThreads;
+  // kept: every key above `prefix`, and the first `left` that equal it.  A thread owns a run of tokens
+  // (an odd number of them: no two threads of a warp on one bank).
+  const int run = ((n + kSelThreads - 1) / kSelThreads) | 1;
   const int j0 = min(n, tid * run), j1 = min(n, j0 + run);
   uint32_t more = 0, same = 0;
   for (int j = j0; j < j1; ++j) {
