@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
 
 // Rows of the survivors to their new pages: a 16-byte piece of K and of V per thread and step, kU steps in flight.
 constexpr int kMoveThreads = 256;
-constexpr int kU = 4;
+constexpr int kU = 2;                   // (8 sequences cut to 8192 tokens: 4 in flight 86 us, 8 104, 2 79)
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictArgs a, int lanes_log2) {
   grid_dependency_wait();
   const int s = blockIdx.z, h = blockIdx.y;
