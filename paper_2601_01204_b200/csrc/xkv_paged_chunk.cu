@@ -66,14 +66,14 @@ __device__ __forceinline__ int seen_by(const PagedAttnArgs& a, const Seq& q, int
 
 // The parts of items in a block's piece, one after the other.
 struct ChunkWalk {
-  uint32_t pos, end, cost;                   // on the line, which has cost + units places per item
+  uint32_t pos, end;                         // on the line, which has kItemCost + units places per item
   Seq q;
   int seq, head, pair, pairs;
   int tile_lo, nt;                           // units [tile_lo, tile_lo + nt) of the item
   int units;                                 // of the item
   int nt0, nt1;                              // of them those of tile 0 and 1
   uint32_t item_lo;                          // the item's place on the line
-  __device__ __forceinline__ void start(uint32_t from, uint32_t to, uint32_t item_cost) { pos = from; end = to; cost = item_cost; seq = -1; }
+  __device__ __forceinline__ void start(uint32_t from, uint32_t to) { pos = from; end = to; seq = -1; }
   __device__ __forceinline__ void open(const ChunkArgs& f) {
     q = seq_at(f.a.cache, f.a.seqs, seq);
     pairs = (q.n_new + 2 * f.tpt - 1) / (2 * f.tpt);
@@ -91,8 +91,8 @@ struct ChunkWalk {
         rel -= (uint32_t)head * per;
         for (pair = 0;; ++pair) {
           units = units_of(seen_by(f.a, q, (pair + 1) * 2 * f.tpt));
-          if (rel < (uint32_t)units + cost) break;
-          rel -= (uint32_t)units + cost;
+          if (rel < (uint32_t)units + kItemCost) break;
+          rel -= (uint32_t)units + kItemCost;
         }
       } else {                               // the next item begins
         rel = 0;
@@ -107,9 +107,9 @@ struct ChunkWalk {
         units = units_of(seen_by(f.a, q, (pair + 1) * 2 * f.tpt));
       }
       item_lo = pos - rel;
-      const uint32_t stop = min((uint32_t)units + cost - rel, end - pos);
-      tile_lo = (int)(max(rel, cost) - cost);
-      nt = (int)(max(rel + stop, cost) - cost) - tile_lo;
+      const uint32_t stop = min((uint32_t)units + kItemCost - rel, end - pos);
+      tile_lo = (int)(max(rel, kItemCost) - kItemCost);
+      nt = (int)(max(rel + stop, kItemCost) - kItemCost) - tile_lo;
       pos += stop;
     } while (nt == 0);                       // (no more than the cost of an item that begins here)
     nt0 = part_of(f, 2 * pair);
@@ -195,7 +195,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   grid_dependency_wait();
-  const uint32_t cost = line_prefix<kThreads>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {
+  line_prefix<kThreads, true>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {
     const Seq q = seq_at(a.cache, a.seqs, s);
     const int pairs = (q.n_new + 2 * f.tpt - 1) / (2 * f.tpt);
     Work w = {(uint32_t)pairs, 0u};
@@ -211,7 +211,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
   const Cut cut(prefix[a.seqs.n_seqs], gridDim.x);
   ChunkWalk walk;
-  walk.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1), cost);
+  walk.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1));
 
   if (warp < kSW) {
     // ============== softmax warps, 16 rows of a tile each ==============
@@ -605,11 +605,11 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       CutItem ci;
       ci.parts = 0;
       ChunkWalk w;
-      w.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1), cost);
+      w.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1));
       for (int part = 0; w.next(f, prefix); ++part) {
         if (w.tile_lo == 0 && w.nt < w.units) {
           ci.row0 = w.q.row0; ci.n_new = w.q.n_new; ci.head = w.head; ci.pair = w.pair;
-          ci.parts = (int)cut.owner(w.item_lo + cost + (uint32_t)w.units - 1) - (int)blockIdx.x + 1;
+          ci.parts = (int)cut.owner(w.item_lo + kItemCost + (uint32_t)w.units - 1) - (int)blockIdx.x + 1;
           ci.slot0 = 2 * blockIdx.x + (part == 0 ? 0 : 1);
         }
       }

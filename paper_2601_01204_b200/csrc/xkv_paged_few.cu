@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   grid_dependency_wait();
-  const uint32_t cost = line_prefix<kThreads>(a.seqs.n_seqs, s_prefix, s_warp, [&](int s) {
+  const uint32_t cost = line_prefix<kThreads, false>(a.seqs.n_seqs, s_prefix, s_warp, [&](int s) {
     const Seq q = seq_at(a.cache, a.seqs, s);
     // (a sequence with new tokens but without cached ones has a unit too: its rows become zero)
     const uint32_t items = q.n_new == 0 ? 0u : (uint32_t)a.cache.n_kv_heads;

@@ -23,45 +23,50 @@ struct Cut {
 
 // What is done once per item (queries, first scores, merging, results) takes as long as some units.  Where a block's piece is long
 // an item therefore has kItemCost more places on the line than it has units, so that blocks with many short items have fewer
-// units; where pieces are a few units only, those count.
+// units; where pieces are a few units only, those count.  (ALWAYS: an item has them anyhow.  The chunk attention's softmax loop is compiled
+// worse with a cost that is not a constant: chunks of four prompts 527 -> 564 us.)
 constexpr uint32_t kItemCost = 2, kLongPiece = 8;
 
 // prefix[s] = places on the line before sequence s, prefix[n_seqs] = all of them; `work` gives a sequence's items and units.  All THREADS
 // threads of the block (a multiple of 32) call it; it ends with a barrier.  Returns the places that an item has more than units.
 struct Work { uint32_t items, units; };
-template <int THREADS, typename F>
+template <int THREADS, bool ALWAYS, typename F>
 __device__ __forceinline__ uint32_t line_prefix(int n_seqs, uint32_t* prefix, uint2* s_warp, F work) {
+  constexpr int kPer = (kMaxSeqs + THREADS - 1) / THREADS;       // sequences of a thread
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (n_seqs + THREADS - 1) / THREADS;
-  uint2 sum = make_uint2(0, 0);
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s >= n_seqs) break;
-    const Work w = work(s);
-    sum.x += w.items; sum.y += w.units;
-  }
-  uint2 inc = sum;
+  Work w[kPer];
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t x = __shfl_up_sync(0xffffffffu, inc.x, o), y = __shfl_up_sync(0xffffffffu, inc.y, o);
-    if (lane >= o) { inc.x += x; inc.y += y; }
+  for (int i = 0; i < kPer; ++i) {
+    const int s = i * THREADS + tid;                             // (in rounds of THREADS sequences)
+    w[i] = s < n_seqs ? work(s) : Work{0u, 0u};
   }
-  if (lane == 31) s_warp[warp] = inc;
-  __syncthreads();
-  uint2 before = make_uint2(inc.x - sum.x, inc.y - sum.y), all = make_uint2(0, 0);
-  for (int w = 0; w < THREADS / 32; ++w) {
-    if (w < warp) { before.x += s_warp[w].x; before.y += s_warp[w].y; }
-    all.x += s_warp[w].x; all.y += s_warp[w].y;
+  uint2 done = make_uint2(0, 0);                                 // of the rounds before
+  uint2 before[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (i > 0 && i * THREADS >= n_seqs) break;
+    uint2 inc = make_uint2(w[i].items, w[i].units);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, inc.x, o), y = __shfl_up_sync(0xffffffffu, inc.y, o);
+      if (lane >= o) { inc.x += x; inc.y += y; }
+    }
+    if (i > 0) __syncthreads();
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    before[i] = make_uint2(done.x + inc.x - w[i].items, done.y + inc.y - w[i].units);
+    for (int v = 0; v < THREADS / 32; ++v) {
+      if (v < warp) { before[i].x += s_warp[v].x; before[i].y += s_warp[v].y; }
+      done.x += s_warp[v].x; done.y += s_warp[v].y;
+    }
   }
-  const uint32_t cost = all.y >= kLongPiece * gridDim.x ? kItemCost : 0;
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s >= n_seqs) break;
-    prefix[s] = before.y + cost * before.x;
-    const Work w = work(s);
-    before.x += w.items; before.y += w.units;
+  const uint32_t cost = ALWAYS || done.y >= kLongPiece * gridDim.x ? kItemCost : 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int s = i * THREADS + tid;
+    if (s < n_seqs) prefix[s] = before[i].y + cost * before[i].x;
   }
-  if (tid == 0) prefix[n_seqs] = all.y + cost * all.x;
+  if (tid == 0) prefix[n_seqs] = done.y + cost * done.x;
   __syncthreads();
   return cost;
 }

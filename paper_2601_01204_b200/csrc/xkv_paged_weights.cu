@@ -145,7 +145,7 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   grid_dependency_wait();
-  line_prefix<kThreads>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {       // (items alone count here: none is cut)
+  line_prefix<kThreads, false>(a.seqs.n_seqs, prefix, s_warp, [&](int s) {       // (items alone count here: none is cut)
     const Seq q = seq_at(a.cache, a.seqs, s);
     seqs[s] = q;
     return Work{0u, q.n_new == 0 ? 0u : (uint32_t)a.cache.n_kv_heads * (uint32_t)((q.len + 2 * kUnit - 1) / (2 * kUnit))};
