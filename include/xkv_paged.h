@@ -136,7 +136,8 @@ XKV_API int kv_paged_append(xkv_paged* cache, const xkv_paged_batch* batch,
  * weights are rounded to the type of v before their product with it, each against a reference maximum of its row.
  * impl: 0 = default, 1 = a simple kernel without tensor cores, kept as a cross-check (fp32 throughout).
  * Values that a token does not see never reach it from behind the end of its sequence, whatever the memory holds there;
- * a non-finite value of a new token may reach the other new tokens of its sequence in the same call. */
+ * a non-finite value of a new token may reach the other new tokens of its sequence in the same call.
+ * Errors: XKV_E_LIMIT if n_seqs * n_kv_heads * (table_width * page_tokens / 128) * (max_new * group / 128) could pass 2^32. */
 XKV_API int attn_paged_causal(xkv_paged* cache, const xkv_paged_batch* batch,
                       const void* q, int64_t q_tok_stride, int64_t q_head_stride,
                       void* out, int64_t o_tok_stride, int64_t o_head_stride,
@@ -146,7 +147,7 @@ XKV_API int attn_paged_causal(xkv_paged* cache, const xkv_paged_batch* batch,
  * over the new tokens and over the query heads of h: exp(q.k * softmax_scale - lse).  q and lse are those of attn_paged_causal
  * with the same mask.  Every slot of every sequence with new tokens is updated.  decay >= 0; with 0 the old
  * weights are not read.  Sums are formed in a fixed order: the same call repeats exactly.
- * A slot that two sequences of the call share gets the update of one of them. */
+ * A slot that two sequences of the call share gets the update of one of them.  Errors: XKV_E_LIMIT as above. */
 XKV_API int kv_paged_weights(xkv_paged* cache, const xkv_paged_batch* batch,
                      const void* q, int64_t q_tok_stride, int64_t q_head_stride, const float* lse,
                      float softmax_scale, float decay, int32_t mask, xkv_stream stream);
@@ -156,9 +157,9 @@ XKV_API int kv_paged_weights(xkv_paged* cache, const xkv_paged_batch* batch,
  * others keep all their tokens.  The survivors' keys, values and weights go, in their order, to slots 0, 1, ... of
  * the pages that dst_table [n_seqs][dst_width] names, which must not be pages that any sequence of the call reads; the old pages
  * stay as they are (they may be shared), the caller frees them.  kept: int32 [n_seqs][n_kv_heads][keep], the
- * survivors' old slots, -1 behind them.  lens_out: int32 [n_seqs], the new lengths, 0 for a sequence that was left out.
+ * survivors' old slots, -1 behind them.  lens_out: int32 [n_seqs], not lens, the new lengths, 0 for a sequence that was left out.
  * Of the batch n_seqs, lens, table and table_width are read.  Errors: XKV_E_INVALID if n_first + n_recent > keep,
- * keep < 1, or dst_width * page_tokens < keep. */
+ * keep < 1, dst_width * page_tokens < keep, lens_out overlaps lens, or dst_table is the batch's table. */
 XKV_API int kv_paged_evict(xkv_paged* cache, const xkv_paged_batch* batch, const int32_t* dst_table, int32_t dst_width,
                    int32_t keep, int32_t n_first, int32_t n_recent, int32_t* kept, int32_t* lens_out, xkv_stream stream);
 

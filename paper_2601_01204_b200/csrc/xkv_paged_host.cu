@@ -300,6 +300,9 @@ int kv_paged_evict(xkv_paged* c, const xkv_paged_batch* b, const int32_t* dst_ta
   if (dst_width < 1 || (int64_t)dst_width * c->p.page_tokens < keep || (int64_t)dst_width * c->p.page_tokens >= ((int64_t)1 << 31) - (1 << 16))
     return XKV_E_INVALID;
   if (!aligned(dst_table, 4) || !aligned(kept, 4) || !aligned(lens_out, 4)) return XKV_E_INVALID;
+  // (blocks of the call read the lengths while others write the new ones)
+  if (lens_out < b->lens + b->n_seqs && b->lens < lens_out + b->n_seqs) return XKV_E_INVALID;
+  if (dst_table == b->table) return XKV_E_INVALID;
   const int rc = on_device(c);
   if (rc != XKV_OK) return rc;
   if (!c->view.weights) return XKV_E_STATE;

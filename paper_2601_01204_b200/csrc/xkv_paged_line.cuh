@@ -23,8 +23,8 @@ struct Cut {
 
 // What is done once per item (queries, first scores, merging, results) takes as long as some units.  Where a block's piece is long
 // an item therefore has kItemCost more places on the line than it has units, so that blocks with many short items have fewer
-// units; where pieces are a few units only, those count.  (ALWAYS: an item has them anyhow.  The chunk attention's softmax loop is compiled
-// worse with a cost that is not a constant: chunks of four prompts 527 -> 564 us.)
+// units; where pieces are a few units only, those count.  (ALWAYS: an item has them anyhow; a constant, which the chunk attention has
+// registers for: chunks of four prompts 532 us instead of 538.)
 constexpr uint32_t kItemCost = 2, kLongPiece = 8;
 
 // prefix[s] = places on the line before sequence s, prefix[n_seqs] = all of them; `work` gives a sequence's items and units.  All THREADS

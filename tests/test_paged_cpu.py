@@ -9,7 +9,7 @@ import pytest
 from paper_2601_01204_b200 import build
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-OK, INVALID, STATE, NOMEM, UNSUPPORTED = 0, -1, -2, -3, -4
+OK, INVALID, STATE, NOMEM, UNSUPPORTED, LIMIT = 0, -1, -2, -3, -4, -7
 A = 1 << 40                                   # an address that nobody reads
 
 
@@ -112,7 +112,7 @@ class Calls:
     def weigh(self, batch=None, q=A, qt=64, qh=512, lse=A, scale=0.125, decay=1.0, mask=0, h=""):
         return self.lib.kv_paged_weights(self.h if h == "" else h, batch or self.batch(), q, qt, qh, lse, scale, decay, mask, None)
 
-    def evict(self, batch=None, dst=A, width=4, keep=40, first=4, recent=8, kept=A, lens=A, h=""):
+    def evict(self, batch=None, dst=A + 4096, width=4, keep=40, first=4, recent=8, kept=A, lens=A + 64, h=""):
         return self.lib.kv_paged_evict(self.h if h == "" else h, batch or self.batch(), dst, width, keep, first, recent, kept, lens, None)
 
 
@@ -191,9 +191,18 @@ def test_weights_refuse(calls, m):
 
 
 @pytest.mark.parametrize("m", [dict(h=None), dict(dst=0), dict(width=2), dict(width=0), dict(width=1 << 27), dict(keep=0), dict(first=-1), dict(recent=-1),
-                               dict(first=30, recent=11), dict(kept=0), dict(lens=0), dict(kept=A + 2)])
+                               dict(first=30, recent=11), dict(kept=0), dict(lens=0), dict(kept=A + 2), dict(lens=A),
+                               dict(lens=A + 4), dict(dst=A)])
 def test_eviction_refuses(calls, m):
     assert calls.evict(**m) == INVALID
+
+
+def test_work_beyond_the_counters_is_refused(calls):
+    big = calls.batch(n_seqs=4, table_width=(1 << 27) - (1 << 13), max_new=1 << 20, n_tokens=1 << 22)
+    n = calls.lib.fake_launches()
+    assert calls.attend(batch=big) == LIMIT and calls.weigh(batch=big) == LIMIT
+    assert calls.lib.fake_launches() == n
+    assert calls.attend(batch=calls.batch(n_seqs=4, table_width=(1 << 27) - (1 << 13), max_new=1)) == OK
 
 
 def test_without_weights(paged, lib):

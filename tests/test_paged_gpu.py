@@ -149,6 +149,60 @@ def test_attention(paged, m, full, impl):
     assert torch.equal(again.view(torch.int16), out.view(torch.int16))
 
 
+@pytest.mark.parametrize("m", [
+    dict(news=[1, 3], lens=[900, 300], heads=4, kv_heads=1), dict(news=[2, 1], lens=[2000, 517], heads=2, kv_heads=2, d=128, dtype="fp16", page=64),
+    dict(news=[100, 37], lens=[1500, 300], heads=4, kv_heads=2, page=32), dict(news=[200], lens=[2100], heads=3, kv_heads=1, dtype="fp16"),
+    dict(news=[130, 257], lens=[900, 2000], heads=2, kv_heads=1, d=128), dict(news=[90], lens=[700], heads=8, kv_heads=2, d=128, dtype="fp16")], ids=str)
+@pytest.mark.parametrize("kind", ["rising", "falling", "steps"])
+@pytest.mark.parametrize("full", [False, True])
+def test_attention_with_moving_maxima(paged, m, kind, full):
+    """Scores that rise along the cache by more than 2^14 in their weights, again and again, for some heads; that fall; that
+    jump inside a unit, differently for neighbouring rows.  (Scaled scores up to 50.)"""
+    w = World(paged, **m)
+    scale = 50.0 / (w.d * w.scale)
+    for b, l in enumerate(w.lens_list):
+        x = torch.arange(l, device="cuda") / l
+        if kind == "falling":
+            x = 1 - x
+        elif kind == "steps":
+            x = ((x * 11).floor() % 4) / 4 + 0.25 * (torch.arange(l, device="cuda") % 97 == 50)
+        w.k[b] = (w.k[b].float() * 0.05 + (x * scale)[None, :, None]).to(w.dt)
+        w.put(b, 0, l)
+    sign = torch.where(torch.arange(w.n, device="cuda") % 3 == 1, -1.0, 1.0)[None, :, None]
+    head = torch.linspace(0.3, 1.0, w.H, device="cuda")[:, None, None]
+    w.q[:, :w.n] = (sign * head + 0.02 * w.q[:, :w.n].float()).to(w.dt)
+    out, lse, (out0, lse0) = w.attend(full)
+    w.check_attention(out, lse, full, out0, lse0)
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+@pytest.mark.parametrize("m", [
+    dict(news=[1] * 1000, lens=[(13 * i) % 61 + 1 for i in range(1000)], heads=2, kv_heads=1),
+    dict(news=[i % 3 for i in range(1024)], lens=[(7 * i) % 40 for i in range(1024)], heads=3, kv_heads=1),
+    dict(news=[(5 * i) % 23 for i in range(700)], lens=[(11 * i) % 90 for i in range(700)], heads=2, kv_heads=2, d=128),
+    dict(news=[0] * 650 + [40, 1], lens=[3] * 650 + [300, 20], heads=2, kv_heads=1, dtype="fp16")], ids=lambda m: f"{len(m['news'])}")
+def test_many_sequences(paged, m):
+    w = World(paged, **m)
+    out, lse, before = w.attend(False)
+    w.check_attention(out, lse, False, *before)
+    ref = lse_of(w, False)
+    old = w.weights.clone()
+    w.cache.kv_paged_weights(w.batch, w.q, ref)
+    for b in range(0, len(w.news), 7):
+        if w.news[b] and w.lens_list[b]:
+            want, room = w.weight_sums(b, False, ref)
+            was = w.get(old, b, w.lens_list[b]).double()
+            assert ((w.get(w.weights, b, w.lens_list[b]).double() - want - was).abs() <= room + 2.0 ** -22 * (want + was)).all(), b
+    k, v = w.tokens(w.K), w.tokens(w.K)
+    w.cache.kv_paged_append(w.batch, k, v)
+    for b in range(0, len(w.news), 5):
+        n = min(w.news[b], w.lens_list[b])
+        if n:
+            rows = slice(w.starts[b] + w.news[b] - n, w.starts[b] + w.news[b])
+            assert torch.equal(w.get(w.k_pages, b, w.lens_list[b])[:, -n:], k[:, rows]) and torch.equal(w.get(w.v_pages, b, w.lens_list[b])[:, -n:], v[:, rows])
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
 # ---- weights ---------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("decay", [1.0, 0.0, 0.75])
@@ -349,6 +403,56 @@ def test_replayed_graph_reads_new_lengths(paged):
             w.v[b] = torch.cat([w.v[b], v[:, b:b + 1]], 1)
             assert torch.equal(w.get(w.v_pages, b, t + 1), w.v[b]) and torch.equal(w.get(w.k_pages, b, t + 1), w.k[b])
         w.check_attention(out, lse, False, out, lse, f"step {t}")
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+def test_replayed_graph_of_a_chunk(paged):
+    """A captured chunk: attention, weights and eviction, replayed with other lengths, tables and tokens in the same places."""
+    w = World(paged, news=[60, 100], lens=[200, 300], heads=4, kv_heads=2, d=128, page=32, spare_pages=8)
+    out, lse = torch.zeros_like(w.q), torch.zeros(w.H, w.rows, device="cuda")
+    dst = w.spare[:8].reshape(2, 4).contiguous()
+    kept, lens_out = torch.zeros(2, w.K, 100, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+
+    def step():
+        w.cache.attn_paged_causal(w.batch, w.q, out=out, lse=lse)
+        w.cache.kv_paged_weights(w.batch, w.q, lse, decay=0.0)
+        w.cache.kv_paged_evict(w.batch, dst, 100, 5, 20, kept=kept, lens_out=lens_out)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    for news, lens, flip in (([60, 100], [200, 300], False), ([10, 3], [180, 299], False), ([100, 60], [300, 200], True), ([0, 100], [17, 100], False)):
+        if flip:
+            w.table.copy_(w.table.flip(0))
+            w.k.reverse(), w.v.reverse()
+        w.q.copy_(w.rand(*w.q.shape))
+        w.news, w.lens_list, w.starts, w.n = news, lens, [0, news[0], sum(news)], sum(news)
+        k, v = list(w.k), list(w.v)
+        w.k, w.v = [x[:, :l] for x, l in zip(k, lens)], [x[:, :l] for x, l in zip(v, lens)]
+        w.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        w.q_start.copy_(torch.tensor(w.starts, dtype=torch.int32))
+        out.fill_(7.0), lse.fill_(7.0)
+        before = out.clone(), lse.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        w.check_attention(out, lse, False, *before)
+        for b in range(2):
+            if news[b]:
+                want, room = w.weight_sums(b, False, lse)
+                got = w.get(w.weights, b, lens[b])
+                assert ((got.double() - want).abs() <= room + 2.0 ** -22 * want).all()
+                for h in range(w.K):
+                    assert kept[b, h, :min(lens[b], 100)].tolist() == chosen(got[h].tolist(), 100, 5, 20)
+        assert lens_out.tolist() == [min(l, 100) for l in lens]
+        w.k, w.v = k, v
+        if flip:
+            w.table.copy_(w.table.flip(0))
+            w.k.reverse(), w.v.reverse()
     assert w.cache.xkv_paged_poll_status() == 0
 
 
