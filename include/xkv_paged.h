@@ -30,6 +30,12 @@ extern "C" {
 
 typedef enum { XKV_BF16 = 0, XKV_FP16 = 1 } xkv_dtype;
 
+/* A token tensor, see above.  (Calls take their token tensors as one array of these: few arguments, which bindings pay for one by one.) */
+typedef struct {
+  const void* data;          /* null: absent, where a call allows that.  Outputs are written through it. */
+  int64_t tok_stride, head_stride;
+} xkv_rows;
+
 /* ---- rotary positions --------------------------------------------------------- */
 
 /* A token at position p has the pairs (x1, x2) of its channels turned:
@@ -53,18 +59,13 @@ typedef struct {
   double  magnitude;         /* > 0, usually 1                                                      */
 } xkv_rotary_params;
 
-/* Turns n tokens of q (n_q_heads heads) and of k (n_k_heads heads, may be 0 with k = null) into q_out and k_out.
- * positions: int32 [n_axes][pos_stride], the first n of each.  An output may be its input (same pointer, same
- * strides); other overlaps are not allowed.  inverse != 0 turns by -a: undoes the rotation (magnitude 1), and takes
- * gradients of the outputs to gradients of the inputs.  n = 0 does nothing.
+/* Turns n tokens of q (n_q_heads heads) and of k (n_k_heads heads; 0: absent) into q_out and k_out.
+ * tensors: q, q_out, k, k_out.  positions: int32 [n_axes][pos_stride], the first n of each.  An output may be its input (same
+ * pointer, same strides); other overlaps are not allowed.  inverse != 0 turns by -a: undoes the rotation (magnitude 1),
+ * and takes gradients of the outputs to gradients of the inputs.  n = 0 does nothing.
  * Errors: XKV_E_INVALID for bad parameters, pointers or strides. */
-XKV_API int xkv_rotary(const xkv_rotary_params* params, int32_t dtype, int32_t head_dim,
-               const int32_t* positions, int64_t pos_stride, int32_t n,
-               const void* q, void* q_out, int32_t n_q_heads, int64_t q_tok_stride, int64_t q_head_stride,
-               int64_t qo_tok_stride, int64_t qo_head_stride,
-               const void* k, void* k_out, int32_t n_k_heads, int64_t k_tok_stride, int64_t k_head_stride,
-               int64_t ko_tok_stride, int64_t ko_head_stride,
-               int32_t inverse, xkv_stream stream);
+XKV_API int xkv_rotary(const xkv_rotary_params* params, int32_t dtype, int32_t head_dim, const int32_t* positions, int64_t pos_stride,
+               int32_t n, const xkv_rows tensors[4], int32_t n_q_heads, int32_t n_k_heads, int32_t inverse, xkv_stream stream);
 
 /* ---- the paged cache ----------------------------------------------------------- */
 
@@ -117,19 +118,15 @@ XKV_API int xkv_paged_create(const xkv_paged_params* params, void* k_pages, void
                      void* dev_workspace, size_t bytes, xkv_stream stream, xkv_paged** out);
 XKV_API int xkv_paged_destroy(xkv_paged* cache);
 
-/* The new tokens into the cache.  k and v (n_kv_heads heads) go to their slots, k turned by `rotary` if that is not
- * null (positions as in xkv_rotary, one column per row), v as it is; the weights of the slots become 0.  If q is not
- * null, q_out receives it turned the same way (or copied); q_out may be q.  New tokens for which the sequence has no slot (more new
+/* The new tokens into the cache.  tensors: k, v, q, q_out.  k and v (n_kv_heads heads) go to their slots, k turned by `rotary` if that is not
+ * null (positions as in xkv_rotary, one column per row), v as it is; the weights of the slots become 0.  If q is
+ * present, q_out receives it turned the same way (or copied); q_out may be q.  New tokens for which the sequence has no slot (more new
  * tokens than lens[b]) are not written.  Slots written by two tokens of a call (two sequences that share the
  * page) hold one of them. */
-XKV_API int kv_paged_append(xkv_paged* cache, const xkv_paged_batch* batch,
-                    const void* k, int64_t k_tok_stride, int64_t k_head_stride,
-                    const void* v, int64_t v_tok_stride, int64_t v_head_stride,
-                    const void* q, int64_t q_tok_stride, int64_t q_head_stride,
-                    void* q_out, int64_t qo_tok_stride, int64_t qo_head_stride,
+XKV_API int kv_paged_append(xkv_paged* cache, const xkv_paged_batch* batch, const xkv_rows tensors[4],
                     const xkv_rotary_params* rotary, const int32_t* positions, int64_t pos_stride, xkv_stream stream);
 
-/* out = softmax(q K^T * softmax_scale) V per head over the tokens that `mask` lets a new token see, and, if lse is not
+/* tensors: q, out.  out = softmax(q K^T * softmax_scale) V per head over the tokens that `mask` lets a new token see, and, if lse is not
  * null, lse[head*n_tokens + row] = log sum exp of its scaled scores (natural logarithm).  The new tokens' own keys and
  * values have to be in the cache (kv_paged_append).  A token that sees nothing (more new tokens than lens[b])
  * gets zeros and an lse of -infinity.  Scores, maxima, sums and accumulators are fp32; the
@@ -138,9 +135,7 @@ XKV_API int kv_paged_append(xkv_paged* cache, const xkv_paged_batch* batch,
  * Values that a token does not see never reach it from behind the end of its sequence, whatever the memory holds there;
  * a non-finite value of a new token may reach the other new tokens of its sequence in the same call.
  * Errors: XKV_E_LIMIT if n_seqs * n_kv_heads * (table_width * page_tokens / 128) * (max_new * group / 128) could pass 2^32. */
-XKV_API int attn_paged_causal(xkv_paged* cache, const xkv_paged_batch* batch,
-                      const void* q, int64_t q_tok_stride, int64_t q_head_stride,
-                      void* out, int64_t o_tok_stride, int64_t o_head_stride,
+XKV_API int attn_paged_causal(xkv_paged* cache, const xkv_paged_batch* batch, const xkv_rows tensors[2],
                       float* lse, float softmax_scale, int32_t mask, int32_t impl, xkv_stream stream);
 
 /* weights[slot of head h] = decay * weights[slot] + the softmax weights that the new tokens gave the slot, added up
@@ -148,8 +143,7 @@ XKV_API int attn_paged_causal(xkv_paged* cache, const xkv_paged_batch* batch,
  * with the same mask.  Every slot of every sequence with new tokens is updated.  decay >= 0; with 0 the old
  * weights are not read.  Sums are formed in a fixed order: the same call repeats exactly.
  * A slot that two sequences of the call share gets the update of one of them.  Errors: XKV_E_LIMIT as above. */
-XKV_API int kv_paged_weights(xkv_paged* cache, const xkv_paged_batch* batch,
-                     const void* q, int64_t q_tok_stride, int64_t q_head_stride, const float* lse,
+XKV_API int kv_paged_weights(xkv_paged* cache, const xkv_paged_batch* batch, const xkv_rows* q, const float* lse,
                      float softmax_scale, float decay, int32_t mask, xkv_stream stream);
 
 /* Every sequence with more than `keep` tokens keeps, per key head, its first n_first and last n_recent tokens and the

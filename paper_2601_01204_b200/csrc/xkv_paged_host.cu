@@ -38,8 +38,11 @@ int device_setup(int* device, int* sm_count) {
 
 bool aligned(const void* p, size_t a) { return p && (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < kMaxStride; }
-// A token tensor of `heads` heads.
-bool tensor_ok(const void* p, int64_t ts, int64_t hs) { return aligned(p, 16) && stride_ok(ts) && stride_ok(hs); }
+bool rows_ok(const xkv_rows& r) { return aligned(r.data, 16) && stride_ok(r.tok_stride) && stride_ok(r.head_stride); }
+// An output may be its input.
+bool in_place_ok(const xkv_rows& in, const xkv_rows& out) {
+  return in.data != out.data || (in.tok_stride == out.tok_stride && in.head_stride == out.head_stride);
+}
 
 int log2_of(int x) {
   int l = 0;
@@ -108,8 +111,11 @@ bool plan_rotary(const xkv_rotary_params* p, int head_dim, bool inverse, const i
   r->magnitude = (float)p->magnitude;
   r->positions = positions; r->pos_stride = pos_stride;
   const double two_pi = 6.283185307179586476925286766559;
-  for (int i = 0; i < r->pairs; ++i) {
-    double w = pow(p->base, -2.0 * i / p->rotary_dim);
+  // (powers one from another in 80 bits: a call of pow for each would take longer than the launch)
+  const long double ratio = powl((long double)p->base, -2.0L / p->rotary_dim);
+  long double power = 1.0L;
+  for (int i = 0; i < r->pairs; ++i, power *= ratio) {
+    double w = (double)power;
     if (p->original_tokens > 0) {
       double keep = (p->original_tokens * w / two_pi - p->beta_slow) / (p->beta_fast - p->beta_slow);
       keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
@@ -122,10 +128,10 @@ bool plan_rotary(const xkv_rotary_params* p, int head_dim, bool inverse, const i
   return true;
 }
 
-TokenTensor token_tensor(const void* in, int64_t its, int64_t ihs, void* out, int64_t ots, int64_t ohs, int heads) {
+TokenTensor token_tensor(const xkv_rows& in, const xkv_rows& out, int heads) {
   TokenTensor t;
-  t.in = reinterpret_cast<const uint8_t*>(in); t.out = reinterpret_cast<uint8_t*>(out);
-  t.in_ts = its; t.in_hs = ihs; t.out_ts = ots; t.out_hs = ohs; t.heads = heads;
+  t.in = reinterpret_cast<const uint8_t*>(in.data); t.out = const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(out.data));
+  t.in_ts = in.tok_stride; t.in_hs = in.head_stride; t.out_ts = out.tok_stride; t.out_hs = out.head_stride; t.heads = heads;
   return t;
 }
 
@@ -145,9 +151,7 @@ int from_cuda(cudaError_t e) {
 extern "C" {
 
 int xkv_rotary(const xkv_rotary_params* params, int32_t dtype, int32_t head_dim, const int32_t* positions, int64_t pos_stride, int32_t n,
-               const void* q, void* q_out, int32_t n_q_heads, int64_t q_ts, int64_t q_hs, int64_t qo_ts, int64_t qo_hs,
-               const void* k, void* k_out, int32_t n_k_heads, int64_t k_ts, int64_t k_hs, int64_t ko_ts, int64_t ko_hs,
-               int32_t inverse, xkv_stream stream) {
+               const xkv_rows* x, int32_t n_q_heads, int32_t n_k_heads, int32_t inverse, xkv_stream stream) {
   if (dtype != XKV_BF16 && dtype != XKV_FP16) return XKV_E_INVALID;
   if (head_dim < 8 || head_dim > 2 * kMaxPairs || head_dim % 8) return XKV_E_INVALID;
   if (n < 0 || n > (1 << 28) || n_q_heads < 1 || n_q_heads > 1024 || n_k_heads < 0 || n_k_heads > 1024) return XKV_E_INVALID;
@@ -155,15 +159,14 @@ int xkv_rotary(const xkv_rotary_params* params, int32_t dtype, int32_t head_dim,
   memset(&a, 0, sizeof(a));
   if (!plan_rotary(params, head_dim, inverse != 0, positions, pos_stride, n, &a.rot)) return XKV_E_INVALID;
   if (n == 0) return XKV_OK;
-  if (!tensor_ok(q, q_ts, q_hs) || !tensor_ok(q_out, qo_ts, qo_hs)) return XKV_E_INVALID;
-  if (n_k_heads > 0 && (!tensor_ok(k, k_ts, k_hs) || !tensor_ok(k_out, ko_ts, ko_hs))) return XKV_E_INVALID;
-  if ((q == q_out && (q_ts != qo_ts || q_hs != qo_hs)) || (n_k_heads > 0 && k == k_out && (k_ts != ko_ts || k_hs != ko_hs))) return XKV_E_INVALID;
+  if (!x || !rows_ok(x[0]) || !rows_ok(x[1]) || !in_place_ok(x[0], x[1])) return XKV_E_INVALID;
+  if (n_k_heads > 0 && (!rows_ok(x[2]) || !rows_ok(x[3]) || !in_place_ok(x[2], x[3]))) return XKV_E_INVALID;
   int dev, sms;
   const int rc = device_setup(&dev, &sms);
   if (rc != XKV_OK) return rc;
   a.n = n; a.head_dim = head_dim;
-  a.q = token_tensor(q, q_ts, q_hs, q_out, qo_ts, qo_hs, n_q_heads);
-  a.k = token_tensor(k, k_ts, k_hs, k_out, ko_ts, ko_hs, n_k_heads);
+  a.q = token_tensor(x[0], x[1], n_q_heads);
+  if (n_k_heads > 0) a.k = token_tensor(x[2], x[3], n_k_heads);
   return from_cuda(launch_tokens(a, dtype, sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 
@@ -233,9 +236,8 @@ int xkv_paged_poll_status(xkv_paged* c, xkv_stream stream) {
   return v;
 }
 
-int kv_paged_append(xkv_paged* c, const xkv_paged_batch* b, const void* k, int64_t k_ts, int64_t k_hs, const void* v, int64_t v_ts, int64_t v_hs,
-                    const void* q, int64_t q_ts, int64_t q_hs, void* q_out, int64_t qo_ts, int64_t qo_hs,
-                    const xkv_rotary_params* rotary, const int32_t* positions, int64_t pos_stride, xkv_stream stream) {
+int kv_paged_append(xkv_paged* c, const xkv_paged_batch* b, const xkv_rows* x, const xkv_rotary_params* rotary, const int32_t* positions,
+                    int64_t pos_stride, xkv_stream stream) {
   if (!c || !batch_ok(c, b, true)) return XKV_E_INVALID;
   TokenArgs a;
   memset(&a, 0, sizeof(a));
@@ -243,30 +245,31 @@ int kv_paged_append(xkv_paged* c, const xkv_paged_batch* b, const void* k, int64
   const int rc = on_device(c);
   if (rc != XKV_OK) return rc;
   if (b->n_tokens == 0) return XKV_OK;
-  if (!tensor_ok(k, k_ts, k_hs) || !tensor_ok(v, v_ts, v_hs)) return XKV_E_INVALID;
-  if (q && (!tensor_ok(q, q_ts, q_hs) || !tensor_ok(q_out, qo_ts, qo_hs) || (q == q_out && (q_ts != qo_ts || q_hs != qo_hs)))) return XKV_E_INVALID;
+  if (!x || !rows_ok(x[0]) || !rows_ok(x[1])) return XKV_E_INVALID;
+  if (x[2].data && (!rows_ok(x[2]) || !rows_ok(x[3]) || !in_place_ok(x[2], x[3]))) return XKV_E_INVALID;
   a.n = b->n_tokens; a.head_dim = c->p.head_dim; a.append = 1;
-  if (q) a.q = token_tensor(q, q_ts, q_hs, q_out, qo_ts, qo_hs, c->p.n_heads);
-  a.k = token_tensor(k, k_ts, k_hs, nullptr, 0, 0, c->p.n_kv_heads);
-  a.v = token_tensor(v, v_ts, v_hs, nullptr, 0, 0, c->p.n_kv_heads);
+  const xkv_rows none = {nullptr, 0, 0};
+  if (x[2].data) a.q = token_tensor(x[2], x[3], c->p.n_heads);
+  a.k = token_tensor(x[0], none, c->p.n_kv_heads);
+  a.v = token_tensor(x[1], none, c->p.n_kv_heads);
   a.cache = c->view; a.seqs = seq_view(b);
   return from_cuda(launch_tokens(a, c->p.dtype, c->sm_count, reinterpret_cast<cudaStream_t>(stream)));
 }
 
-int attn_paged_causal(xkv_paged* c, const xkv_paged_batch* b, const void* q, int64_t q_ts, int64_t q_hs, void* out, int64_t o_ts, int64_t o_hs,
-                      float* lse, float scale, int32_t mask, int32_t impl, xkv_stream stream) {
+int attn_paged_causal(xkv_paged* c, const xkv_paged_batch* b, const xkv_rows* x, float* lse, float scale, int32_t mask, int32_t impl,
+                      xkv_stream stream) {
   if (!c || !batch_ok(c, b, true) || !(scale > 0.f) || !isfinite(scale) || (mask != XKV_MASK_CAUSAL && mask != XKV_MASK_FULL) || (impl != 0 && impl != 1))
     return XKV_E_INVALID;
   const int rc = on_device(c);
   if (rc != XKV_OK) return rc;
   if (b->n_tokens == 0 || b->max_new == 0) return XKV_OK;
-  if (!tensor_ok(q, q_ts, q_hs) || !tensor_ok(out, o_ts, o_hs) || (lse && !aligned(lse, 4))) return XKV_E_INVALID;
+  if (!x || !rows_ok(x[0]) || !rows_ok(x[1]) || (lse && !aligned(lse, 4))) return XKV_E_INVALID;
   PagedAttnArgs a;
   memset(&a, 0, sizeof(a));
   a.cache = c->view; a.seqs = seq_view(b);
-  a.q = reinterpret_cast<const uint8_t*>(q); a.q_ts = q_ts; a.q_hs = q_hs;
-  a.out = reinterpret_cast<uint8_t*>(out); a.o_ts = o_ts; a.o_hs = o_hs;
-  a.lse = lse; a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f; a.full = mask == XKV_MASK_FULL;
+  a.q = reinterpret_cast<const uint8_t*>(x[0].data); a.q_ts = x[0].tok_stride; a.q_hs = x[0].head_stride;
+  a.out = const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(x[1].data)); a.o_ts = x[1].tok_stride; a.o_hs = x[1].head_stride;
+  a.lse = lse; a.scale_log2 = scale * 1.4426950408889634f; a.full = mask == XKV_MASK_FULL;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (impl == 1) return from_cuda(launch_paged_attn_simple(a, c->p.head_dim, c->p.dtype, st));
   if (!work_ok(c, b)) return XKV_E_LIMIT;
@@ -275,19 +278,19 @@ int attn_paged_causal(xkv_paged* c, const xkv_paged_batch* b, const void* q, int
   return from_cuda(launch_attn_chunk(a, c->maps_page, c->scratch, c->cuts, c->p.head_dim, c->p.dtype, c->sm_count, st));
 }
 
-int kv_paged_weights(xkv_paged* c, const xkv_paged_batch* b, const void* q, int64_t q_ts, int64_t q_hs, const float* lse, float scale, float decay,
-                     int32_t mask, xkv_stream stream) {
+int kv_paged_weights(xkv_paged* c, const xkv_paged_batch* b, const xkv_rows* q, const float* lse, float scale, float decay, int32_t mask,
+                     xkv_stream stream) {
   if (!c || !batch_ok(c, b, true) || !(scale > 0.f) || !isfinite(scale) || !(decay >= 0.f) || !isfinite(decay) ||
       (mask != XKV_MASK_CAUSAL && mask != XKV_MASK_FULL)) return XKV_E_INVALID;
   const int rc = on_device(c);
   if (rc != XKV_OK) return rc;
   if (!c->view.weights) return XKV_E_STATE;
   if (b->n_tokens == 0 || b->max_new == 0 || b->table_width == 0) return XKV_OK;
-  if (!tensor_ok(q, q_ts, q_hs) || !aligned(lse, 4)) return XKV_E_INVALID;
+  if (!q || !rows_ok(*q) || !aligned(lse, 4)) return XKV_E_INVALID;
   PagedWeightArgs a;
   memset(&a, 0, sizeof(a));
   a.cache = c->view; a.seqs = seq_view(b);
-  a.q = reinterpret_cast<const uint8_t*>(q); a.q_ts = q_ts; a.q_hs = q_hs;
+  a.q = reinterpret_cast<const uint8_t*>(q->data); a.q_ts = q->tok_stride; a.q_hs = q->head_stride;
   a.lse = lse; a.scale_log2 = scale * 1.4426950408889634f; a.decay = decay; a.full = mask == XKV_MASK_FULL;
   if (!work_ok(c, b)) return XKV_E_LIMIT;
   return from_cuda(launch_paged_weights(a, c->maps_page, c->p.head_dim, c->p.dtype, c->sm_count, reinterpret_cast<cudaStream_t>(stream)));

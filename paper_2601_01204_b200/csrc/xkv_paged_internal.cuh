@@ -109,7 +109,7 @@ struct PagedAttnArgs {
   const uint8_t* q; int64_t q_ts, q_hs;
   uint8_t* out; int64_t o_ts, o_hs;
   float* lse;
-  float scale, scale_log2;
+  float scale_log2;
   int full;                              // every token of the sequence is seen
 };
 

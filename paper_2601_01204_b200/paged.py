@@ -7,6 +7,7 @@ used for device memory and streams.  There is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from dataclasses import dataclass, field
 
 from .xkv import XKV_E_INVALID, XkvError, _i32, _i64, _sz, _vp, lib
@@ -40,9 +41,9 @@ class xkv_paged_batch(C.Structure):
 _f = C.c_float
 _batch = C.POINTER(xkv_paged_batch)
 _rotary = C.POINTER(xkv_rotary_params)
+_rows_of = C.c_char_p            # an array of xkv_rows, packed
 lib.xkv_rotary.restype = C.c_int
-lib.xkv_rotary.argtypes = [_rotary, _i32, _i32, _vp, _i64, _i32, _vp, _vp, _i32, _i64, _i64, _i64, _i64,
-                           _vp, _vp, _i32, _i64, _i64, _i64, _i64, _i32, _vp]
+lib.xkv_rotary.argtypes = [_rotary, _i32, _i32, _vp, _i64, _i32, _rows_of, _i32, _i32, _i32, _vp]
 lib.xkv_paged_workspace_bytes.restype = _sz
 lib.xkv_paged_workspace_bytes.argtypes = [C.POINTER(xkv_paged_params), _i32]
 lib.xkv_paged_create.restype = C.c_int
@@ -50,16 +51,20 @@ lib.xkv_paged_create.argtypes = [C.POINTER(xkv_paged_params), _vp, _vp, _vp, _vp
 lib.xkv_paged_destroy.restype = C.c_int
 lib.xkv_paged_destroy.argtypes = [_vp]
 lib.kv_paged_append.restype = C.c_int
-lib.kv_paged_append.argtypes = [_vp, _batch, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64,
-                                _rotary, _vp, _i64, _vp]
+lib.kv_paged_append.argtypes = [_vp, _batch, _rows_of, _rotary, _vp, _i64, _vp]
 lib.attn_paged_causal.restype = C.c_int
-lib.attn_paged_causal.argtypes = [_vp, _batch, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _f, _i32, _i32, _vp]
+lib.attn_paged_causal.argtypes = [_vp, _batch, _rows_of, _vp, _f, _i32, _i32, _vp]
 lib.kv_paged_weights.restype = C.c_int
-lib.kv_paged_weights.argtypes = [_vp, _batch, _vp, _i64, _i64, _vp, _f, _f, _i32, _vp]
+lib.kv_paged_weights.argtypes = [_vp, _batch, _rows_of, _vp, _f, _f, _i32, _vp]
 lib.kv_paged_evict.restype = C.c_int
 lib.kv_paged_evict.argtypes = [_vp, _batch, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp]
 lib.xkv_paged_poll_status.restype = C.c_int
 lib.xkv_paged_poll_status.argtypes = [_vp, _vp]
+
+
+# xkv_rows: data, tok_stride, head_stride, of one, two or four token tensors
+_pack1, _pack2, _pack4 = (struct.Struct(f"{3 * n}q").pack for n in (1, 2, 4))
+_ABSENT = (0, 0, 0)
 
 
 def _refuse(where: str, what: str) -> None:
@@ -164,18 +169,18 @@ def xkv_rotary(params: RotaryParams, positions, q, k=None, q_out=None, k_out=Non
     H, n, d = shape
     if q_out is None:
         q_out = torch.empty_like(q)
-    pq, qt, qh = _rows(q, where, "q", device, dtype, shape)
-    po, ot, oh = _rows(q_out, where, "q_out", device, dtype, shape)
-    pk = pko = kt = kh = kot = koh = K = 0
+    rq, ro = _rows(q, where, "q", device, dtype, shape), _rows(q_out, where, "q_out", device, dtype, shape)
+    rk = rko = _ABSENT
+    K = 0
     if k is not None:
         K = k.shape[0]
         if k_out is None:
             k_out = torch.empty_like(k)
-        pk, kt, kh = _rows(k, where, "k", device, dtype, (K, n, d))
-        pko, kot, koh = _rows(k_out, where, "k_out", device, dtype, (K, n, d))
+        shape = (K, n, d)
+        rk, rko = _rows(k, where, "k", device, dtype, shape), _rows(k_out, where, "k_out", device, dtype, shape)
     pp, ps = _positions(positions, where, device, params.n_axes, n)
-    _call(device, lib.xkv_rotary, where, params.ref, BF16 if dtype == _bf16 else FP16, d, pp, ps, n, pq, po, H, qt, qh, ot, oh,
-          pk, pko, K, kt, kh, kot, koh, 1 if inverse else 0)
+    _call(device, lib.xkv_rotary, where, params.ref, BF16 if dtype == _bf16 else FP16, d, pp, ps, n, _pack4(*rq, *ro, *rk, *rko),
+          H, K, 1 if inverse else 0)
     return q_out, k_out
 
 
@@ -266,22 +271,20 @@ class PagedCache:
         where = "kv_paged_append"
         device, dtype = self.device, self.dtype
         shape = self._shape(where, batch, self.p.n_kv_heads)
-        pk, kt, kh = _rows(k, where, "k", device, dtype, shape)
-        pv, vt, vh = _rows(v, where, "v", device, dtype, shape)
-        pq = po = qt = qh = ot = oh = pp = ps = 0
+        rk, rv = _rows(k, where, "k", device, dtype, shape), _rows(v, where, "v", device, dtype, shape)
+        rq = ro = _ABSENT
         if q is not None:
             shape = (self.p.n_heads, batch.n_tokens, self.p.head_dim)
-            pq, qt, qh = _rows(q, where, "q", device, dtype, shape)
             if q_out is None:
                 q_out = _torch.empty_like(q)
-            po, ot, oh = _rows(q_out, where, "q_out", device, dtype, shape)
-        ref = None
+            rq, ro = _rows(q, where, "q", device, dtype, shape), _rows(q_out, where, "q_out", device, dtype, shape)
+        ref, pp, ps = None, 0, 0
         if rotary is not None:
             if positions is None:
                 _refuse(where, "rotary needs positions")
             pp, ps = _positions(positions, where, device, rotary.n_axes, batch.n_tokens)
             ref = rotary.ref
-        _call(device, lib.kv_paged_append, where, self.handle, batch.ref, pk, kt, kh, pv, vt, vh, pq, qt, qh, po, ot, oh, ref, pp, ps)
+        _call(device, lib.kv_paged_append, where, self.handle, batch.ref, _pack4(*rk, *rv, *rq, *ro), ref, pp, ps)
         return q_out
 
     def attn_paged_causal(self, batch: PagedBatch, q, out=None, lse=None, scale: float | None = None, mask: int = MASK_CAUSAL,
@@ -290,12 +293,11 @@ class PagedCache:
         [n_heads][n_tokens], contiguous) is filled if given.  Returns out."""
         where = "attn_paged_causal"
         shape = self._shape(where, batch, self.p.n_heads)
-        pq, qt, qh = _rows(q, where, "q", self.device, self.dtype, shape)
         if out is None:
             out = _torch.zeros_like(q)        # rows that belong to nobody are not written
-        po, ot, oh = _rows(out, where, "out", self.device, self.dtype, shape)
+        rq, ro = _rows(q, where, "q", self.device, self.dtype, shape), _rows(out, where, "out", self.device, self.dtype, shape)
         pl = 0 if lse is None else self._lse(lse, where, shape)
-        _call(self.device, lib.attn_paged_causal, where, self.handle, batch.ref, pq, qt, qh, po, ot, oh, pl,
+        _call(self.device, lib.attn_paged_causal, where, self.handle, batch.ref, _pack2(*rq, *ro), pl,
               self.scale if scale is None else scale, mask, impl)
         return out
 
@@ -309,8 +311,8 @@ class PagedCache:
         in attn_paged_causal)."""
         where = "kv_paged_weights"
         shape = self._shape(where, batch, self.p.n_heads)
-        pq, qt, qh = _rows(q, where, "q", self.device, self.dtype, shape)
-        _call(self.device, lib.kv_paged_weights, where, self.handle, batch.ref, pq, qt, qh, self._lse(lse, where, shape),
+        rq = _rows(q, where, "q", self.device, self.dtype, shape)
+        _call(self.device, lib.kv_paged_weights, where, self.handle, batch.ref, _pack1(*rq), self._lse(lse, where, shape),
               self.scale if scale is None else scale, decay, mask)
 
     def kv_paged_evict(self, batch: PagedBatch, dst_table, keep: int, n_first: int = 0, n_recent: int = 0, kept=None, lens_out=None):

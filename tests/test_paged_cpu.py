@@ -2,6 +2,7 @@
 import ctypes as C
 import os
 import re
+import struct
 import subprocess
 
 import pytest
@@ -83,6 +84,11 @@ def test_create_refuses_pointers(paged, lib):
     assert lib.xkv_paged_workspace_bytes(C.byref(p), 0) == 0
 
 
+def rows(*tensors):
+    """An array of xkv_rows."""
+    return struct.pack(f"{len(tensors)}q", *tensors)
+
+
 class Calls:
     """The calls with arguments that are in order, each of which a test can put out of order."""
 
@@ -103,14 +109,14 @@ class Calls:
         return C.byref(self.paged.xkv_rotary_params(*[v[n] for n, _ in self.paged.xkv_rotary_params._fields_]))
 
     def append(self, batch=None, k=A, kt=64, kh=512, v=A, vt=64, vh=512, q=A, qt=64, qh=512, o=A + 4096, ot=64, oh=512, rot="", pos=A, ps=5, h=""):
-        return self.lib.kv_paged_append(self.h if h == "" else h, batch or self.batch(), k, kt, kh, v, vt, vh, q, qt, qh, o, ot, oh,
+        return self.lib.kv_paged_append(self.h if h == "" else h, batch or self.batch(), rows(k, kt, kh, v, vt, vh, q, qt, qh, o, ot, oh),
                                         self.rotary() if rot == "" else rot, pos, ps, None)
 
     def attend(self, batch=None, q=A, qt=64, qh=512, o=A, ot=64, oh=512, lse=A, scale=0.125, mask=0, impl=0, h=""):
-        return self.lib.attn_paged_causal(self.h if h == "" else h, batch or self.batch(), q, qt, qh, o, ot, oh, lse, scale, mask, impl, None)
+        return self.lib.attn_paged_causal(self.h if h == "" else h, batch or self.batch(), rows(q, qt, qh, o, ot, oh), lse, scale, mask, impl, None)
 
     def weigh(self, batch=None, q=A, qt=64, qh=512, lse=A, scale=0.125, decay=1.0, mask=0, h=""):
-        return self.lib.kv_paged_weights(self.h if h == "" else h, batch or self.batch(), q, qt, qh, lse, scale, decay, mask, None)
+        return self.lib.kv_paged_weights(self.h if h == "" else h, batch or self.batch(), rows(q, qt, qh), lse, scale, decay, mask, None)
 
     def evict(self, batch=None, dst=A + 4096, width=4, keep=40, first=4, recent=8, kept=A, lens=A + 64, h=""):
         return self.lib.kv_paged_evict(self.h if h == "" else h, batch or self.batch(), dst, width, keep, first, recent, kept, lens, None)
@@ -147,6 +153,10 @@ def test_calls_without_work_launch_nothing(calls):
     assert calls.attend(batch=calls.batch(max_new=0)) == OK
     assert calls.weigh(batch=empty, q=0) == OK
     assert calls.lib.fake_launches() == n
+    assert calls.lib.kv_paged_append(calls.h, calls.batch(), None, None, None, 0, None) == INVALID
+    assert calls.lib.attn_paged_causal(calls.h, calls.batch(), None, A, 1.0, 0, 0, None) == INVALID
+    assert calls.lib.kv_paged_weights(calls.h, calls.batch(), None, A, 1.0, 1.0, 0, None) == INVALID
+    assert calls.lib.fake_launches() == n
     assert calls.append() == OK and calls.append(q=0) == OK and calls.append(rot=None, pos=0) == OK
     assert calls.attend() == OK and calls.attend(lse=0) == OK and calls.attend(impl=1, mask=1) == OK
     assert calls.weigh() == OK and calls.evict() == OK
@@ -165,13 +175,13 @@ def test_append_refuses(calls, m):
 def test_rotary_parameters_are_refused(calls, m):
     r = calls.rotary(**m)
     assert calls.append(rot=r) == INVALID
-    assert calls.lib.xkv_rotary(r, 0, 64, A, 5, 5, A, A, 2, 64, 512, 64, 512, None, None, 0, 0, 0, 0, 0, 0, None) == INVALID
+    assert calls.lib.xkv_rotary(r, 0, 64, A, 5, 5, rows(A, 64, 512, A, 64, 512, 0, 0, 0, 0, 0, 0), 2, 0, 0, None) == INVALID
 
 
 def test_rotary_refuses(calls):
     def call(dtype=0, d=64, pos=A, ps=5, n=5, q=A, o=A, heads=2, qt=64, qh=512, ot=64, oh=512, k=A, ko=A, kheads=2, kt=64, kh=512, kot=64, koh=512, **m):
-        return calls.lib.xkv_rotary(calls.rotary(rotary_dim=32, **m), dtype, d, pos, ps, n, q, o, heads, qt, qh, ot, oh, k, ko, kheads,
-                                    kt, kh, kot, koh, 0, None)
+        return calls.lib.xkv_rotary(calls.rotary(rotary_dim=32, **m), dtype, d, pos, ps, n, rows(q, qt, qh, o, ot, oh, k, kt, kh, ko, kot, koh),
+                                    heads, kheads, 0, None)
     assert call() == OK and call(k=0, ko=0, kheads=0) == OK and call(n=0, q=0, pos=0) == OK and call(n_axes=2) == OK
     for m in (dict(dtype=2), dict(d=60), dict(d=256), dict(d=16), dict(n=-1), dict(pos=0), dict(q=0), dict(o=0), dict(heads=0), dict(qt=4),
               dict(k=0), dict(ko=A + 8), dict(kt=0), dict(ot=128), dict(koh=1024), dict(kheads=-1), dict(n_axes=2, ps=4)):
