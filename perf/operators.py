@@ -198,7 +198,8 @@ def prepare(case, seed):
         s["positions"] = pos.to(torch.int32)
     if case["op"] == "rotary":
         if own:
-            s["rotary"] = _own_rotary(case)
+            import paper_2601_01204_b200.paged as paged
+            s["rotary"], s["turn"] = _own_rotary(case), paged.xkv_rotary
         return s
 
     # the pages: every sequence has its own, in no order; those of the eviction's targets behind them
@@ -268,8 +269,7 @@ def _own_run(s):
     case = s["case"]
     op = case["op"]
     if op == "rotary":
-        import paper_2601_01204_b200.paged as paged
-        paged.xkv_rotary(s["rotary"], s["positions"], s["q"], s["k"], q_out=s["q_out"], k_out=s["k_out"])
+        s["turn"](s["rotary"], s["positions"], s["q"], s["k"], q_out=s["q_out"], k_out=s["k_out"])
         return s["q_out"], s["k_out"]
     if op == "append":
         s["cache"].kv_paged_append(s["batch"], s["k"], s["v"], q=s["q"], q_out=s["q_out"], rotary=s["rotary"], positions=s["positions"])
