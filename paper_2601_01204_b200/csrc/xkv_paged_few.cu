@@ -22,6 +22,7 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kStep = 16;                                  // tokens of a warp's step
+constexpr int kSeqsHeld = 64;                              // sequences whose numbers stay in shared memory (the others' are read again)
 constexpr int kMergeFloats = kWarps * kFewRows * 40;       // 16 rows of 32 channels and 8 of padding (no bank conflicts) per warp
 
 template <int D> struct Few {
@@ -68,14 +69,14 @@ struct FewWalk {
   uint32_t item_lo;                      // the item's place on the line
   int key0, key1;                        // tokens of the part
   bool whole;                            // it is all of its item
-  __device__ __forceinline__ bool next(const FewArgs& f, const uint32_t* prefix) {
+  __device__ __forceinline__ bool next(const FewArgs& f, const uint32_t* prefix, const Seq* held) {
     int units;
     do {
       if (pos >= end) return false;
       uint32_t rel = 0;
       if (seq < 0 || pos >= prefix[seq + 1]) {
         seq = line_seq(prefix, f.a.seqs.n_seqs, pos);
-        const Seq q = seq_at(f.a.cache, f.a.seqs, seq);
+        const Seq q = seq < kSeqsHeld ? held[seq] : seq_at(f.a.cache, f.a.seqs, seq);
         len = q.len; row0 = q.row0; n_new = q.n_new;
         per = cost + (uint32_t)max(1, (len + kUnit - 1) / kUnit);
         rel = pos - prefix[seq];
@@ -105,6 +106,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
   __shared__ __align__(16) float s_merge[kMergeFloats];
   __shared__ float2 s_ml[kWarps][kFewRows];
   __shared__ uint32_t s_prefix[kMaxSeqs + 1];
+  __shared__ Seq s_seq[kSeqsHeld];
   __shared__ uint2 s_warp[kWarps];
   __shared__ uint32_t s_abort, s_last;
   const PagedAttnArgs& a = f.a;
@@ -121,6 +123,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
   grid_dependency_wait();
   const uint32_t cost = line_prefix<kThreads, false>(a.seqs.n_seqs, s_prefix, s_warp, [&](int s) {
     const Seq q = seq_at(a.cache, a.seqs, s);
+    if (s < kSeqsHeld) s_seq[s] = q;
     // (a sequence with new tokens but without cached ones has a unit too: its rows become zero)
     const uint32_t items = q.n_new == 0 ? 0u : (uint32_t)a.cache.n_kv_heads;
     return Work{items, items * (uint32_t)max(1, (q.len + kUnit - 1) / kUnit)};
@@ -137,13 +140,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
   // ---- copies: this warp's steps of all parts, kStages of them ahead ----
   FewWalk ahead = walk;
   int a_key = 0;                          // next step's first token
-  bool a_more = ahead.next(f, s_prefix);
+  bool a_more = ahead.next(f, s_prefix, s_seq);
   if (a_more) a_key = ahead.key0 + kStep * warp;
   int ids = 0, id_key = -1;               // pages of this lane's step among the next 32 (lane l: l * kWarps steps on)
   uint32_t put = 0;                       // steps asked for
   auto ask = [&]() {                      // the next step's copies, if there is one
     while (a_more && a_key >= ahead.key1) {
-      a_more = ahead.next(f, s_prefix);
+      a_more = ahead.next(f, s_prefix, s_seq);
       if (a_more) a_key = ahead.key0 + kStep * warp;
       id_key = -1;
     }
@@ -175,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
   const int g = lane >> 2, t = lane & 3;
   uint32_t got = 0;                       // steps consumed
   int part = 0;
-  for (; walk.next(f, s_prefix); ++part) {
+  for (; walk.next(f, s_prefix, s_seq); ++part) {
     const int rows = walk.n_new * a.cache.group;
     // ---- queries: rows g and g + 8 of the item, row r = (new token r / group, head r mod group) ----
     uint32_t qf[D / 16][4];
@@ -333,13 +336,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
     if (whole) continue;
     // ---- an item that several blocks share: the last to arrive merges the pieces in their order ----
     const uint32_t first = cut.owner(walk.item_lo + cost), parts = cut.owner(walk.item_lo + walk.per - 1) - first + 1;
+    // (the barrier before orders this block's partial results before the addition, the one behind it the others' after it)
     if (tid == 0) {
-      __threadfence();
-      s_last = atomicAdd(&f.s.count[first], 1u) == parts - 1;
+      uint32_t before;
+      asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(f.s.count + first) : "memory");
+      s_last = before == parts - 1;
     }
     __syncthreads();
     if (!s_last) continue;
-    __threadfence();
     // (in the block where it starts the item may follow another one)
     const uint32_t slot0 = 2 * first + (cut.start(first) < walk.item_lo ? 1 : 0);
     // Threads take (row, 4 channels); where there are fewer of those than threads, groups of threads share out the pieces
