@@ -21,10 +21,12 @@ struct Cut {
   }
 };
 
-// What is done once per item (queries, first scores, merging, results) takes as long as some units.  Where a block's piece is long
-// an item therefore has kItemCost more places on the line than it has units, so that blocks with many short items have fewer
-// units; where pieces are a few units only, those count.  (ALWAYS: an item has them anyhow; a constant, which the chunk attention has
-// registers for: chunks of four prompts 532 us instead of 538.)
+// What is done once per item (queries, first scores, merging, results) takes as long as some units.  An item therefore has kItemCost
+// more places on the line than units, so that blocks with many short items have fewer units.  (Chunks of four prompts 617 us
+// without, 583 with 2, 585 with 4, at that time; 64 decoding sequences 154 -> 111 together with a shorter merge.  A unit of an item
+// that has one tile alone takes as long as one of two: counted as half, a frame over 16384 tokens 136 -> 164 us.)
+// Where pieces are a few units only, those count, and items cost nothing, unless ALWAYS: a constant, which the chunk attention has
+// registers for (532 us instead of 538).
 constexpr uint32_t kItemCost = 2, kLongPiece = 8;
 
 // prefix[s] = places on the line before sequence s, prefix[n_seqs] = all of them; `work` gives a sequence's items and units.  All THREADS
