@@ -127,10 +127,17 @@ __device__ __forceinline__ uint64_t mul_f2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ float max_nan(float a, float b) {         // NaN if either is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
 // 2^x of two numbers on the FMA pipes, for a share of the exponentials where the special-function unit is what bounds a kernel: x = n + r
 // with n the nearest whole number, a polynomial in r whose relative error on [-1/2, 1/2] is minimax (coefficients by the
-// Remez exchange), and n added to the exponent's bits.  Relative error 2.1e-7 (degree 5), 2.7e-6 (4), 7.5e-5 (3) in fp32.
-// Arguments below -126 count as -126, above 127 are not for this function.
+// Remez exchange), times 2^n.  Relative error 2.1e-7 (degree 5), 2.7e-6 (4), 7.5e-5 (3) in fp32.
+// Outside its range it answers as fast_exp2 does, so that it makes no difference which of them a number meets: a NaN stays one,
+// results below 2^-126 are 0 (n is -127 at least, whose scale is 0), from 127.5 on they are infinite (n counts as 128 at most; that is
+// done on its bits, one instruction with the sum: on x it costs the weights of a frame 2 %).  +infinity itself gives a NaN.
 template <int DEGREE>
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
   constexpr float kMagic = 12582912.f;       // 1.5 * 2^23: adding it rounds to a whole number, in the low bits of the sum
@@ -138,15 +145,17 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
                              {0.9999992847442627f, 0.6931217908859253f, 0.240247443318367f, 0.05591785907745361f, 0.009570102207362652f, 0.f},
                              {1.0000001192092896f, 0.6931469440460205f, 0.24022120237350464f, 0.05550713092088699f, 0.009675540961325169f,
                               0.0013276472454890609f}};
-  x = pack_f2(fmaxf(f2_lo(x), -126.f), fmaxf(f2_hi(x), -126.f));
+  x = pack_f2(max_nan(f2_lo(x), -127.f), max_nan(f2_hi(x), -127.f));
   const uint64_t t = add_f2(x, pack_f2(kMagic, kMagic));
   const uint64_t n = add_f2(t, pack_f2(-kMagic, -kMagic));
   const uint64_t r = fma_f2(n, pack_f2(-1.f, -1.f), x);
   uint64_t p = pack_f2(c[DEGREE - 3][DEGREE], c[DEGREE - 3][DEGREE]);
 #pragma unroll
   for (int i = DEGREE - 1; i >= 0; --i) p = fma_f2(p, r, pack_f2(c[DEGREE - 3][i], c[DEGREE - 3][i]));
-  return pack_f2(__uint_as_float((uint32_t)p + ((uint32_t)t << 23)),
-                 __uint_as_float((uint32_t)(p >> 32) + ((uint32_t)(t >> 32) << 23)));
+  auto scale = [](uint32_t bits) { return __uint_as_float((uint32_t)__viaddmin_s32((int)bits, 127 - 0x4B400000, 255) << 23); };
+  uint64_t y;
+  asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(y) : "l"(p), "l"(pack_f2(scale((uint32_t)t), scale((uint32_t)(t >> 32)))));
+  return y;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
