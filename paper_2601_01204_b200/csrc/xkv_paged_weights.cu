@@ -195,8 +195,8 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
           __syncwarp();
           tc_fence_after();
           // columns [lo, cols) see the token: tokens i >= token - base; columns behind the tile's rows belong to nobody
-          const int lo = a.full ? 0 : (token - base - tok0) * G;
           const bool all = a.full || walk.first + kUnit * (int)u + kUnit - 1 <= base + tok0;      // (the same in all threads)
+          const int lo = all ? 0 : (token - base - tok0) * G;      // (of a unit far behind the new tokens the product could pass 32 bits)
           uint64_t sum = 0ull, sum1 = 0ull;
 #pragma unroll 1
           for (int c0 = 0; c0 < cols; c0 += 32) {

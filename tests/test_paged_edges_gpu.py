@@ -69,3 +69,29 @@ def test_weights_outside_the_range(paged, m, full):
     s, _ = w.scores(0, full)
     low = s.masked_fill(torch.isneginf(s), math.inf).amin()     # every score that is seen has a weight above exp(100) > 2^128
     assert torch.isinf(weigh(w, torch.full_like(lse, low.item() - 100.0), full)).all()
+
+
+# ---- weights: a cache whose length times the rows of a token passes 2^31 ------------------------
+
+def test_weights_of_a_very_long_cache(paged):
+    """34 304 000 tokens (all but the first page's are one page, again and again), 63 heads on one key head."""
+    G, d, P, again = 63, 64, 256, 133999
+    length = P * (again + 1)
+    assert (length - 1) * G > 2 ** 31
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    kp, vp = (torch.randn(2, 1, P, d, device="cuda", generator=gen).bfloat16() for _ in range(2))
+    weights = torch.zeros(2, 1, P, device="cuda")
+    cache = paged.PagedCache(paged.PagedParams(G, 1, d, P, 2, 1), kp, vp, weights)
+    table = torch.ones(1, again + 1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    batch = paged.PagedBatch(torch.tensor([0, 1], dtype=torch.int32, device="cuda"),
+                             torch.tensor([length], dtype=torch.int32, device="cuda"), table, 1, 1)
+    q = torch.randn(G, 1, d, device="cuda", generator=gen).bfloat16()
+    s = torch.einsum("gd,ptd->gpt", q[:, 0].double(), kp[:, 0].double()) * d ** -0.5
+    lse = torch.log(torch.exp(s[:, 0]).sum(-1) + again * torch.exp(s[:, 1]).sum(-1))[:, None]
+    cache.kv_paged_weights(batch, q, lse.float(), decay=0.0)
+    assert cache.xkv_paged_poll_status() == 0
+    want = torch.exp(s - lse[..., None]).sum(0)                 # (the second page's slots are written many times, with the same)
+    size = torch.einsum("gd,ptd->gpt", q[:, 0].double().abs(), kp[:, 0].double().abs()).amax().item() * d ** -0.5
+    delta = (d + 4) * 2.0 ** -24 * size + 2.0 ** -20
+    assert ((weights[:, 0].double() - want).abs() <= (delta + 2.0 ** -16 + 2.0 ** -22) * want).all()
