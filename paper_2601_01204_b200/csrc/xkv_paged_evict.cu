@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
   auto key_on = [&](int page, int j) {                // key of middle token j on that page
     if ((unsigned)page < (unsigned)a.cache.n_pages) return order_key(a.cache.weights[weight_offset(a.cache, page, h, lo + j)]);
     paged_report(a.cache.status, (int)XKV_E_INVALID);
-    return 0u;
+    return order_key(0.f);                            // a page that does not exist reads as zero
   };
   const int in_smem = min(n, held);
   constexpr int kAhead = 8;                           // tokens of a thread whose pages, and then weights, are asked for at once
@@ -169,7 +169,14 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
     const int slot = kept[i];
     const int src = page_at(a.cache, a.seqs.table, a.seqs.table_width, s, slot);
     const int dst = page_at(a.cache, a.dst_table, a.dst_width, s, i);
-    if (src < 0 || dst < 0) continue;
+    if (dst < 0) continue;
+    if (src < 0) {                                       // a page that does not exist reads as zero
+      const int64_t at = 2 * row_offset(a.cache, dst, h, i) + 16 * piece;
+      *reinterpret_cast<uint4*>(a.cache.k + at) = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(a.cache.v + at) = make_uint4(0, 0, 0, 0);
+      if (piece == 0) a.cache.weights[weight_offset(a.cache, dst, h, i)] = 0.f;
+      continue;
+    }
     const int64_t from = 2 * row_offset(a.cache, src, h, slot) + 16 * piece;
     k[u] = *reinterpret_cast<const uint4*>(a.cache.k + from);
     v[u] = *reinterpret_cast<const uint4*>(a.cache.v + from);

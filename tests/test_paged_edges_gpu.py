@@ -95,3 +95,42 @@ def test_weights_of_a_very_long_cache(paged):
     size = torch.einsum("gd,ptd->gpt", q[:, 0].double().abs(), kp[:, 0].double().abs()).amax().item() * d ** -0.5
     delta = (d + 4) * 2.0 ** -24 * size + 2.0 ** -20
     assert ((weights[:, 0].double() - want).abs() <= (delta + 2.0 ** -16 + 2.0 ** -22) * want).all()
+
+
+# ---- pages that do not exist read as zero --------------------------------------------------------
+
+def without_page(w, b, at):
+    """Entry `at` of sequence b's table names no page; the world's own copy of those tokens becomes zero."""
+    w.table[b, at] = w.p.n_pages + 5
+    lo, hi = at * w.P, min((at + 1) * w.P, w.lens_list[b])
+    w.k[b][:, lo:hi] = 0
+    w.v[b][:, lo:hi] = 0
+    return lo, hi
+
+
+@pytest.mark.parametrize("page", [16, 64])
+def test_evict_from_a_page_that_is_not_there(paged, page):
+    """Its tokens have weight 0, and those that are kept are zeros in the new pages."""
+    l, keep, recent = 6 * page, 5 * page, 5
+    first = 2 * page + page // 2                                # half of the missing page is protected
+    w = World(paged, news=[0], lens=[l], page=page, spare_pages=8)
+    x = torch.rand(l, w.K, device="cuda", generator=w.gen) + 0.5
+    x[::2] *= -1
+    at, place = w.pages_of(torch.arange(l, device="cuda"), 0)
+    w.weights[at, :, place] = x
+    k, v = w.k[0].clone(), w.v[0].clone()
+    lo, hi = 2 * page, 3 * page
+    w.table[0, 2] = w.p.n_pages
+    k[:, lo:hi], v[:, lo:hi], x[lo:hi] = 0, 0, 0
+    dst = w.spare[:5].reshape(1, 5).contiguous()
+    kept, lens_out = w.cache.kv_paged_evict(w.batch, dst, keep, first, recent)
+    assert w.cache.xkv_paged_poll_status() == -1 and lens_out.tolist() == [keep]
+    for h in range(w.K):
+        middle = sorted(range(first, l - recent), key=lambda j: (-x[j, h].item(), j))[:keep - first - recent]
+        want = sorted(list(range(first)) + middle + list(range(l - recent, l)))
+        assert any(lo <= j < hi for j in middle) and not all(j in middle for j in range(first, l - recent) if x[j, h] < 0)
+        assert kept[0, h].tolist() == want
+        idx = torch.tensor(want, device="cuda")
+        for pool, old in ((w.k_pages, k), (w.v_pages, v)):
+            assert torch.equal(bits(w.get(pool, 0, keep, dst)[h]), bits(old[h][idx]))
+        assert torch.equal(w.get(w.weights, 0, keep, dst)[h], x[:, h][idx])
