@@ -394,8 +394,10 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
           for (int g = 0; g < 8; ++g) {
             const float x0 = __uint_as_float(ro[4 * g]) * inv0, x1 = __uint_as_float(ro[4 * g + 1]) * inv0;
             const float x2 = __uint_as_float(ro[4 * g + 2]) * inv1, x3 = __uint_as_float(ro[4 * g + 3]) * inv1;
-            if (has_a) *reinterpret_cast<uint32_t*>(oa + 16 * g) = BF16 ? pack_bf2(x0, x1) : pack_h2(x0, x1);
-            if (has_b) *reinterpret_cast<uint32_t*>(ob + 16 * g) = BF16 ? pack_bf2(x2, x3) : pack_h2(x2, x3);
+            const uint32_t wa = BF16 ? pack_bf2(x0, x1) : pack_h2(x0, x1), wb = BF16 ? pack_bf2(x2, x3) : pack_h2(x2, x3);
+            // (a row that sees nothing is zero, whatever a weight of 0 met)
+            if (has_a) *reinterpret_cast<uint32_t*>(oa + 16 * g) = s0 == 0.f ? 0u : wa;
+            if (has_b) *reinterpret_cast<uint32_t*>(ob + 16 * g) = s1 == 0.f ? 0u : wb;
           }
         } else {
           float* dst = f.s.o + prow * D + c + cq2;

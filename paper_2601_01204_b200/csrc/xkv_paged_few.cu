@@ -320,6 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
           x.x += wgt * y.x; x.y += wgt * y.y; x.z += wgt * y.z; x.w += wgt * y.w;
         }
         if (whole) {
+          if (sum == 0.f) x = make_float4(0.f, 0.f, 0.f, 0.f);       // (a row that sees nothing, whatever a weight of 0 met)
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
           const int n = r / a.cache.group, hq = walk.head * a.cache.group + (r - n * a.cache.group);
           uint2 out;
@@ -407,6 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
         __syncthreads();
       }
       if (grp == 0 && i < work) {
+        if (sum == 0.f) x = make_float4(0.f, 0.f, 0.f, 0.f);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const int n = r / a.cache.group, hq = walk.head * a.cache.group + (r - n * a.cache.group);
         uint2 out;

@@ -134,3 +134,23 @@ def test_evict_from_a_page_that_is_not_there(paged, page):
         for pool, old in ((w.k_pages, k), (w.v_pages, v)):
             assert torch.equal(bits(w.get(pool, 0, keep, dst)[h]), bits(old[h][idx]))
         assert torch.equal(w.get(w.weights, 0, keep, dst)[h], x[:, h][idx])
+
+
+# ---- attention: rows that see nothing-------------------------------------------------------------
+
+@pytest.mark.parametrize("m", [
+    dict(news=[6], lens=[2], heads=2, kv_heads=2), dict(news=[3, 2], lens=[1, 40], heads=4, kv_heads=1, d=128, dtype="fp16"),
+    dict(news=[150], lens=[100], heads=5, kv_heads=1), dict(news=[200, 40], lens=[199, 20], heads=2, kv_heads=2, d=128),
+    dict(news=[700, 300], lens=[500, 200], heads=16, kv_heads=16, dtype="fp16")], ids=str)
+@pytest.mark.parametrize("impl", [1, 0])
+def test_rows_without_a_token_beside_values_that_are_not_finite(paged, m, impl):
+    w = World(paged, **m)
+    for b, l in enumerate(w.lens_list):
+        w.v[b][:, :, ::2] = math.nan
+        w.v[b][:, :, 1::2] = math.inf
+        w.put(b, 0, l)
+    out, lse, _ = w.attend(impl=impl)
+    for b, (n, l) in enumerate(zip(w.news, w.lens_list)):
+        rows = slice(w.starts[b], w.starts[b] + max(0, n - l))
+        assert (out[:, rows] == 0).all() and torch.isneginf(lse[:, rows]).all()
+    assert w.cache.xkv_paged_poll_status() == 0
