@@ -25,13 +25,19 @@ __global__ void __launch_bounds__(128) paged_attn_simple_kernel(const __grid_con
   grid_dependency_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = blockIdx.x * 4 + warp, g = blockIdx.y;
-  int lo = 0, hi = a.seqs.n_seqs;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.seqs.q_start[mid] <= row) lo = mid; else hi = mid;
+  // the sequence whose row this is; all are looked at, so that one with numbers out of bounds hides no other
+  int lo = -1;
+  for (int s0 = 0; s0 < a.seqs.n_seqs; s0 += 32) {
+    bool mine = false;
+    if (s0 + lane < a.seqs.n_seqs) {
+      const Seq x = seq_at(a.cache, a.seqs, s0 + lane);
+      mine = row >= x.row0 && row < x.row0 + x.n_new;
+    }
+    const uint32_t who = __ballot_sync(0xffffffffu, mine);
+    if (who) lo = s0 + __ffs(who) - 1;
   }
+  if (lo < 0) return;
   const Seq q = seq_at(a.cache, a.seqs, lo);
-  if (row < q.row0 || row >= q.row0 + q.n_new) return;
   const int seen = a.full ? q.len : max(0, q.len - q.n_new + (row - q.row0) + 1);
   const int h = g / a.cache.group;
   const uint8_t* qp = a.q + 2 * ((int64_t)g * a.q_hs + (int64_t)row * a.q_ts);

@@ -58,11 +58,27 @@ __global__ void __launch_bounds__(kThreads, 4) tokens_kernel(const __grid_consta
   __shared__ float2 s_cs[kMaxTok][kMaxPairs];
   __shared__ int64_t s_page[kMaxTok];         // row offset of the token's slot at head 0, -1: not written, -2: nobody's row
   __shared__ int64_t s_weight[kMaxTok];
+  __shared__ int s_seq[kMaxTok], s_slot[kMaxTok];      // sequence of a token, -1: nobody's; its slot there, may be negative
+  const int tid = threadIdx.x;
+  if (APPEND) {
+    if (tid < kMaxTok) s_seq[tid] = -1;
+    __syncthreads();
+  }
   grid_dependency_wait();
   const int tok0 = blockIdx.x * d.per;
   const int toks = min(d.per, a.n - tok0);
   const int all_pairs = a.rot.axes * a.rot.pairs;
-  const int tid = threadIdx.x;
+  if (APPEND) {
+    // Every sequence looks for its rows in the block, so that one with numbers out of bounds hides no other (and its loads are one
+    // behind another at most: a search through q_start would take one for every halving).
+    for (int s = tid; s < a.seqs.n_seqs; s += kThreads) {
+      const Seq q = seq_at(a.cache, a.seqs, s);
+      for (int t = max(0, q.row0 - tok0); t < min(toks, q.row0 + q.n_new - tok0); ++t) {
+        s_seq[t] = s;
+        s_slot[t] = q.len - q.n_new + (tok0 + t - q.row0);
+      }
+    }
+  }
   for (int e = tid; e < toks * all_pairs; e += kThreads) {
     const int t = e / all_pairs, p = e - t * all_pairs;
     const int axis = p / a.rot.pairs, i = p - axis * a.rot.pairs;
@@ -72,24 +88,13 @@ __global__ void __launch_bounds__(kThreads, 4) tokens_kernel(const __grid_consta
     sincospif(2.f * (float)part, &s, &c);
     s_cs[t][p] = make_float2(c * a.rot.magnitude, s * a.rot.magnitude);
   }
-  if (APPEND && tid < toks) {
-    const int row = tok0 + tid;
-    // the sequence whose rows hold this one: the last with q_start <= row
-    int lo = 0, hi = a.seqs.n_seqs;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.seqs.q_start[mid] <= row) lo = mid; else hi = mid;
-    }
-    const Seq q = seq_at(a.cache, a.seqs, lo);
-    s_page[tid] = -2;
-    if (row >= q.row0 && row < q.row0 + q.n_new) {
-      s_page[tid] = -1;
-      const int slot = q.len - q.n_new + (row - q.row0);
-      const int page = slot >= 0 ? page_at(a.cache, a.seqs.table, a.seqs.table_width, lo, slot) : -1;
-      if (page >= 0) {
-        s_page[tid] = row_offset(a.cache, page, 0, slot);
-        s_weight[tid] = weight_offset(a.cache, page, 0, slot);
-      }
+  if (APPEND) {
+    __syncthreads();
+    if (tid < toks) {
+      const int seq = s_seq[tid], slot = s_slot[tid];
+      const int page = seq >= 0 && slot >= 0 ? page_at(a.cache, a.seqs.table, a.seqs.table_width, seq, slot) : -1;
+      s_page[tid] = seq < 0 ? -2 : page < 0 ? -1 : row_offset(a.cache, page, 0, slot);
+      if (page >= 0) s_weight[tid] = weight_offset(a.cache, page, 0, slot);
     }
   }
   __syncthreads();

@@ -154,3 +154,37 @@ def test_rows_without_a_token_beside_values_that_are_not_finite(paged, m, impl):
         rows = slice(w.starts[b], w.starts[b] + max(0, n - l))
         assert (out[:, rows] == 0).all() and torch.isneginf(lse[:, rows]).all()
     assert w.cache.xkv_paged_poll_status() == 0
+
+
+@pytest.mark.parametrize("start", [1, 2])
+def test_append_beside_a_sequence_out_of_bounds(paged, start):
+    """A row number beyond the tensors in the middle of q_start: both sequences that it bounds are left out, no other."""
+    w = World(paged, news=[2, 30, 9, 1, 5], lens=[50, 90, 20, 7, 64], pad=4)
+    w.q_start[start] = 10 ** 6
+    good = [b for b in range(5) if b not in (start - 1, start)]
+    k, v = w.tokens(w.K), w.tokens(w.K)
+    q_out = torch.full_like(w.q, 7.0)
+    pools = w.k_pages.clone()
+    w.cache.kv_paged_append(w.batch, k, v, q=w.q, q_out=q_out)
+    assert w.cache.xkv_paged_poll_status() == -1
+    written = torch.zeros(pools.shape[:3], dtype=torch.bool, device="cuda")
+    for b in range(5):
+        rows, n = slice(w.starts[b], w.starts[b] + w.news[b]), w.news[b]
+        if b in good:
+            assert torch.equal(w.get(w.k_pages, b, w.lens_list[b])[:, -n:], k[:, rows]), b
+            assert torch.equal(w.get(w.v_pages, b, w.lens_list[b])[:, -n:], v[:, rows]), b
+            assert torch.equal(q_out[:, rows], w.q[:, rows]), b
+            page, place = w.pages_of(torch.arange(w.lens_list[b] - n, w.lens_list[b], device="cuda"), b)
+            written[page, :, place] = True
+        else:
+            assert (q_out[:, rows] == 7.0).all(), b
+    assert ((w.k_pages == pools) | (w.k_pages.isnan() & pools.isnan()))[~written].all()
+    news = list(w.news)
+    for b in range(5):
+        w.k[b], w.v[b] = w.get(w.k_pages, b, w.lens_list[b]), w.get(w.v_pages, b, w.lens_list[b])
+    for impl in (1, 0):
+        w.news = news
+        out, lse, before = w.attend(impl=impl)
+        assert w.cache.xkv_paged_poll_status() == -1
+        w.news = [n if b in good else 0 for b, n in enumerate(news)]
+        w.check_attention(out, lse, False, *before, tag=f"impl {impl}")
