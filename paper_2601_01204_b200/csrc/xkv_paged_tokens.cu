@@ -55,7 +55,7 @@ struct Deal {
 
 template <typename T, Layout L, bool APPEND>
 __global__ void __launch_bounds__(kThreads, 4) tokens_kernel(const __grid_constant__ TokenArgs a, const __grid_constant__ Deal d) {
-  __shared__ float2 s_cs[kMaxTok][kMaxPairs];
+  __shared__ __align__(16) float2 s_cs[kMaxTok][kMaxPairs];        // (read two pairs at a time)
   __shared__ int64_t s_page[kMaxTok];         // row offset of the token's slot at head 0, -1: not written, -2: nobody's row
   __shared__ int64_t s_weight[kMaxTok];
   __shared__ int s_seq[kMaxTok], s_slot[kMaxTok];      // sequence of a token, -1: nobody's; its slot there, may be negative

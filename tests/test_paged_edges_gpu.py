@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from paged_testlib import World, lse_of
+from paged_testlib import DTYPE, HALF, World, lse_of, turned
 
 pytestmark = pytest.mark.gpu
 
@@ -153,6 +153,67 @@ def test_rows_without_a_token_beside_values_that_are_not_finite(paged, m, impl):
     for b, (n, l) in enumerate(zip(w.news, w.lens_list)):
         rows = slice(w.starts[b], w.starts[b] + max(0, n - l))
         assert (out[:, rows] == 0).all() and torch.isneginf(lse[:, rows]).all()
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+# ---- rotary and append in blocks of two, four and eight tokens -------------------------------------
+
+MANY = [dict(rot=64), dict(rot=64, interleaved=True), dict(rot=32, axes=2), dict(rot=6, axes=3), dict(rot=10, interleaved=True)]
+
+
+@pytest.mark.parametrize("n", [600, 1300, 5000])
+@pytest.mark.parametrize("layout", ["head", "token"])
+@pytest.mark.parametrize("m", MANY, ids=str)
+def test_rotary_of_many_tokens(paged, m, n, layout):
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    for d, heads, k_heads, dtype in ((64, 7, 2, "bf16"), (128, 5, 0, "fp16")):
+        def make(h):
+            x = torch.randn((h, n, d) if layout == "head" else (n, h, d), device="cuda", generator=gen).to(DTYPE[dtype])
+            return x if layout == "head" else x.transpose(0, 1)
+        q, k = make(heads), make(k_heads) if k_heads else None
+        pos = torch.randint(0, 100000, (m.get("axes", 1), n), device="cuda", generator=gen).to(torch.int32)
+        outs = paged.xkv_rotary(paged.RotaryParams(m["rot"], m.get("axes", 1), m.get("interleaved", False)), pos, q, k)
+        for x, got in zip((q, k), outs):
+            if x is None:
+                continue
+            want, room = turned(x, pos, **m)
+            assert ((got.double() - want).abs() <= HALF[DTYPE[dtype]] * want.abs() + room * 1.01 + (2.0 ** -25 if dtype == "fp16" else 0.0)).all()
+            keep = m["rot"] * m.get("axes", 1)
+            assert torch.equal(got[..., keep:], x[..., keep:])
+
+
+@pytest.mark.parametrize("n", [600, 1300, 5000])
+@pytest.mark.parametrize("layout", ["head", "token"])
+@pytest.mark.parametrize("m", MANY[:4], ids=str)
+def test_append_of_many_tokens(paged, m, n, layout):
+    news = [n // 3, 0, n - n // 3 - 40, 1, 39]
+    w = World(paged, news=news, lens=[x + 37 * i for i, x in enumerate(news)], heads=6, kv_heads=3, page=32, order="slot" if layout == "token" else "head",
+              layout=layout, pad=11)
+    k, v = w.tokens(w.K), w.tokens(w.K)
+    pos = torch.randint(0, 100000, (m.get("axes", 1), w.rows), device="cuda", generator=w.gen).to(torch.int32)
+    pools = [x.clone() for x in (w.k_pages, w.v_pages, w.weights)]
+    q_out = torch.full_like(w.q, 7.0)
+    w.cache.kv_paged_append(w.batch, k, v, q=w.q, q_out=q_out, positions=pos,
+                            rotary=paged.RotaryParams(m["rot"], m.get("axes", 1), m.get("interleaved", False)))
+    h = HALF[w.dt]
+    want_k, room_k = turned(k, pos, **m)
+    want_q, room_q = turned(w.q, pos, **m)
+    ours = slice(0, w.n)
+    assert ((q_out[:, ours].double() - want_q[:, ours]).abs() <= h * want_q[:, ours].abs() + room_q[:, ours] * 1.01).all()
+    assert (q_out[:, w.n:] == 7.0).all()
+    written = torch.zeros_like(w.weights, dtype=torch.bool)
+    for b, (c, l) in enumerate(zip(w.news, w.lens_list)):
+        if not c:
+            continue
+        rows = slice(w.starts[b], w.starts[b] + c)
+        page, place = w.pages_of(torch.arange(l - c, l, device="cuda"), b)
+        written[page, :, place] = True
+        got = w.k_pages[page, :, place].transpose(0, 1).double()
+        assert ((got - want_k[:, rows]).abs() <= h * want_k[:, rows].abs() + room_k[:, rows] * 1.01).all()
+        assert torch.equal(w.v_pages[page, :, place].transpose(0, 1), v[:, rows])
+        assert (w.weights[page, :, place] == 0).all()
+    for now, before in zip((w.k_pages, w.v_pages, w.weights), pools):
+        assert ((now == before) | (now.isnan() & before.isnan()))[~written].all()
     assert w.cache.xkv_paged_poll_status() == 0
 
 
