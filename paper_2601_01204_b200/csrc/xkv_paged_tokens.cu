@@ -132,8 +132,7 @@ __global__ void __launch_bounds__(kThreads, 4) tokens_kernel(const __grid_consta
   const int step = kThreads >> d.items_log2;
   constexpr int kU = L == kPairs ? 8 : 4;                // rows in flight per thread
   const int h_lo = blockIdx.y * d.share;                 // blockIdx.y: a share of the heads
-  const int h_n = min(d.share, heads - h_lo);
-  const int total = h_n << d.per_log2;
+  const int total = d.share << d.per_log2;               // (of the last share some may be none: `heads` ends it)
   for (int base = tid >> d.items_log2; base < total; base += kU * step) {
     uint4 x0[kU], x1[L == kPairs ? 1 : kU];
     uint8_t* dst[kU];
