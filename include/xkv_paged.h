@@ -132,8 +132,9 @@ XKV_API int kv_paged_append(xkv_paged* cache, const xkv_paged_batch* batch, cons
  * gets zeros and an lse of -infinity.  Scores, maxima, sums and accumulators are fp32; the
  * weights are rounded to the type of v before their product with it, each against a reference maximum of its row.
  * impl: 0 = default, 1 = a simple kernel without tensor cores, kept as a cross-check (fp32 throughout).
- * Values that a token does not see never reach it from behind the end of its sequence, whatever the memory holds there;
- * a non-finite value of a new token may reach the other new tokens of its sequence in the same call.
+ * Values that a token does not see never reach it, whatever they are: NaN and infinities of later tokens, and what the memory
+ * holds behind the end of its sequence.  (A token before a value that is not finite may be computed a second time, by a slow
+ * kernel.)  out may be q where all values are finite.
  * Errors: XKV_E_LIMIT if n_seqs * n_kv_heads * (table_width * page_tokens / 128) * (max_new * group / 128) could pass 2^32. */
 XKV_API int attn_paged_causal(xkv_paged* cache, const xkv_paged_batch* batch, const xkv_rows tensors[2],
                       float* lse, float softmax_scale, int32_t mask, int32_t impl, xkv_stream stream);

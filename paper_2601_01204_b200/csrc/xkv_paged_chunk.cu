@@ -22,8 +22,17 @@
 // Measured: a frame of 1374 queries over 16384 tokens, 16 heads of 64, 135 us (680 TFLOP/s; the exponentials alone need 80); chunks of
 // four prompts, 32 / 8 heads of 128, 525 us (1.01 PFLOP/s).  What bounds it is the chain scores -> exponentials -> P -> accumulator.
 //
+// Values that are not finite.  P is 0 where a row does not see a token, and 0 times a NaN or an infinity of V is a NaN: a new token's
+// value that is not finite would reach the tokens before it.  A softmax warp that writes a NaN behind a finite sum
+// marks the sequence, and the merge looks at the rows of marked sequences again, and at rows that it merged to a NaN: those whose NaN can be
+// the work of tokens that they do not see are computed once more, a warp per row, from the tokens that they see.  (That is slow,
+// some microseconds a row; without a mark it costs a maximum per word that is written, and the merge one look at a word.)
+//
 // Every wait is bounded (see mbar_wait); when one runs out the block carries on without waiting and reports XKV_E_TIMEOUT.
+#include <type_traits>
+
 #include "xkv_paged_line.cuh"
+#include "xkv_paged_row.cuh"
 #include "xkv_ptx.cuh"
 
 namespace xkv {
@@ -50,7 +59,7 @@ template <int D> struct Chunk {
 };
 
 // What is needed to merge an item whose units several blocks share; written by the block it starts in.
-struct CutItem { int row0, n_new, head, pair, parts, slot0, pad0, pad1; };
+struct CutItem { int row0, n_new, head, pair, parts, slot0, seq, pad; };
 
 struct ChunkArgs {
   PagedAttnArgs a;
@@ -135,6 +144,20 @@ __device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int
 __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int c, int head, int tok, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                ::"r"(dst), "l"(map), "r"(c), "r"(head), "r"(tok), "r"(bar) : "memory");
+}
+
+// Maxima of two pairs of 16-bit numbers, NaN where either is.
+template <bool BF16>
+__device__ __forceinline__ uint32_t max_nan_pair(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ bool any_nan(uint32_t x) {
+  constexpr uint32_t kInf = BF16 ? 0x7F80u : 0x7C00u;
+  return (x & 0x7FFFu) > kInf || ((x >> 16) & 0x7FFFu) > kInf;
 }
 
 // O *= alpha for the calling warp's 16 rows (two per thread); a real call, to keep its registers out of the softmax loop.
@@ -377,6 +400,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       }
       const int head_a = walk.head * G + r % G, head_b = walk.head * G + (r + 8) % G;
       const int64_t row_a = walk.q.row0 + tok_a, row_b = walk.q.row0 + tok_b;
+      uint32_t nan_a = 0u, nan_b = 0u;              // NaN if an output of the row is
 #pragma unroll 1
       for (int c = 0; c < D; c += 64) {
         uint32_t ro[32];
@@ -398,6 +422,8 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
             // (a row that sees nothing is zero, whatever a weight of 0 met)
             if (has_a) *reinterpret_cast<uint32_t*>(oa + 16 * g) = s0 == 0.f ? 0u : wa;
             if (has_b) *reinterpret_cast<uint32_t*>(ob + 16 * g) = s1 == 0.f ? 0u : wb;
+            nan_a = max_nan_pair<BF16>(nan_a, wa);
+            nan_b = max_nan_pair<BF16>(nan_b, wb);
           }
         } else {
           float* dst = f.s.o + prow * D + c + cq2;
@@ -408,6 +434,10 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
           }
         }
       }
+      // (not of the last new token, which sees all, nor where the sum says as much, or nothing was seen; of a frame all tokens see all)
+      if (whole && !a.full && ((any_nan<BF16>(nan_a) && s0 > 0.f && has_a && tok_a + 1 < walk.q.n_new) ||
+                               (any_nan<BF16>(nan_b) && s1 > 0.f && has_b && tok_b + 1 < walk.q.n_new)))
+        f.s.again[0] = f.s.again[2 + walk.seq] = 1u;
       if ((lane & 3) == 0) {
         if (!whole) { f.s.ml[prow] = make_float2(m0, s0); f.s.ml[prow + 8] = make_float2(m1, s1); }
         else if (a.lse) {
@@ -613,7 +643,7 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
       w.start(cut.start(blockIdx.x), cut.start(blockIdx.x + 1));
       for (int part = 0; w.next(f, prefix); ++part) {
         if (w.tile_lo == 0 && w.nt < w.units) {
-          ci.row0 = w.q.row0; ci.n_new = w.q.n_new; ci.head = w.head; ci.pair = w.pair;
+          ci.row0 = w.q.row0; ci.n_new = w.q.n_new; ci.head = w.head; ci.pair = w.pair; ci.seq = w.seq;
           ci.parts = (int)cut.owner(w.item_lo + kItemCost + (uint32_t)w.units - 1) - (int)blockIdx.x + 1;
           ci.slot0 = 2 * blockIdx.x + (part == 0 ? 0 : 1);
         }
@@ -631,19 +661,64 @@ attn_chunk_kernel(const __grid_constant__ ChunkArgs f, const __grid_constant__ P
   }
 }
 
+// Rows of a marked sequence again, a warp per row.  What the row's output holds as NaN may come from values that the row does not see: if new
+// tokens behind it have values there that are not finite, and no token up to it has a NaN there, which the output would have to show.
+template <typename T, int D>
+__device__ __noinline__ void look_again(const ChunkArgs& f, int seq, int tok, int g, float* s_q) {
+  const PagedAttnArgs& a = f.a;
+  const Seq q = seq_at(a.cache, a.seqs, seq);
+  const int lane = threadIdx.x & 31, row = q.row0 + tok, h = g / a.cache.group;
+  const int seen = q.len - q.n_new + tok + 1;
+  if (seen <= 0) return;                               // zero, as it should be
+  constexpr int kWords = D / 64;                       // channels 2 lane + 64 i and the next
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  constexpr uint32_t kExp = kBf16 ? 0x7F807F80u : 0x7C007C00u;
+  auto special = [&](uint32_t w, bool nan) {           // of the two numbers of a word, bits 0 and 16: not finite, or NaN
+    const uint32_t e = w & kExp, f2 = w & ~kExp & 0x7FFF7FFFu;
+    const bool lo = (e & 0xFFFFu) == (kExp & 0xFFFFu) && (!nan || (f2 & 0xFFFFu)), hi = (e >> 16) == (kExp >> 16) && (!nan || (f2 >> 16));
+    return (lo ? 1u : 0u) | (hi ? 0x10000u : 0u);
+  };
+  const uint8_t* op = a.out + 2 * ((int64_t)g * a.o_hs + (int64_t)row * a.o_ts);
+  auto words = [&](int slot, uint32_t (&w)[kWords]) {  // of a value
+    const int page = page_at(a.cache, a.seqs.table, a.seqs.table_width, seq, slot);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i)
+      w[i] = page < 0 ? 0u : *reinterpret_cast<const uint32_t*>(a.cache.v + 2 * row_offset(a.cache, page, h, slot) + 4 * (lane + 32 * i));
+  };
+  uint32_t open = 0;                                   // of this lane's channels those in question, word i's at bits i and 16 + i
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) open |= special(*reinterpret_cast<const uint32_t*>(op + 4 * (lane + 32 * i)), true) << i;
+  if (!__any_sync(0xffffffffu, open != 0)) return;
+  uint32_t from = 0;
+#pragma unroll 4
+  for (int j = seen; j < q.len; ++j) {
+    uint32_t w[kWords];
+    words(j, w);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) from |= special(w[i], false) << i;
+  }
+  open &= from;
+  for (int j = seen - 1; j >= max(0, q.len - q.n_new); --j) {
+    if (!__any_sync(0xffffffffu, open != 0)) return;
+    uint32_t w[kWords];
+    words(j, w);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) open &= ~(special(w[i], true) << i);
+  }
+  if (__any_sync(0xffffffffu, open != 0)) attend_row<T, D>(a, seq, q, row, g, s_q);
+}
+
 // Merge of the items that were cut between blocks, in the order of the pieces: 32 rows per block, (row, 8 channels) per thread.
 constexpr int kMergeRows = 32;
+// Answers whether the row is to be looked at again, as above.
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kMergeRows * D / 8) chunk_merge_kernel(const __grid_constant__ ChunkArgs f) {
-  grid_dependency_wait();
-  const CutItem ci = f.cuts[blockIdx.y];
-  if (ci.parts == 0) return;
+__device__ __forceinline__ bool merge_rows(const ChunkArgs& f, const CutItem& ci) {
   const PagedAttnArgs& a = f.a;
   const int G = a.cache.group;
   const int t = (int)blockIdx.x / (128 / kMergeRows);
   const int r = ((int)blockIdx.x % (128 / kMergeRows)) * kMergeRows + (int)threadIdx.x / (D / 8), c = ((int)threadIdx.x % (D / 8)) * 8;
   const int tok = (2 * ci.pair + t) * f.tpt + r / G;
-  if (r >= f.tpt * G || tok >= ci.n_new) return;
+  if (r >= f.tpt * G || tok >= ci.n_new) return false;
   float m = -INFINITY, l = 0.f;
   float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int p0 = 0; p0 < ci.parts; p0 += 4) {
@@ -687,6 +762,56 @@ __global__ void __launch_bounds__(kMergeRows * D / 8) chunk_merge_kernel(const _
   for (int i = 0; i < 4; ++i) o[i] = BF16 ? pack_bf2(acc[2 * i] * inv, acc[2 * i + 1] * inv) : pack_h2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
   *reinterpret_cast<uint4*>(a.out + 2 * (head * a.o_hs + row * a.o_ts + c)) = make_uint4(o[0], o[1], o[2], o[3]);
   if (c == 0 && a.lse) a.lse[head * a.seqs.n_tokens + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  bool strange = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) strange |= any_nan<BF16>(o[i]);
+  return strange && !a.full && l > 0.f && tok + 1 < ci.n_new;
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kMergeRows * D / 8) chunk_merge_kernel(const __grid_constant__ ChunkArgs f) {
+  grid_dependency_wait();
+  using T = typename std::conditional<BF16, __nv_bfloat16, __half>::type;
+  constexpr int kWarps = kMergeRows * D / 8 / 32;
+  __shared__ float s_q[kWarps][D];
+  __shared__ bool s_last;
+  const CutItem ci = f.cuts[blockIdx.y];
+  const bool again = f.s.again[0] != 0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = f.a.cache.group;
+  // (the barrier makes the merged rows visible to the warps that look at them again)
+  if (ci.parts != 0 && __syncthreads_or(merge_rows<D, BF16>(f, ci))) {
+    const int t = (int)blockIdx.x / (128 / kMergeRows), r0 = ((int)blockIdx.x % (128 / kMergeRows)) * kMergeRows;
+    for (int r = r0 + warp; r < r0 + kMergeRows; r += kWarps) {
+      const int tok = (2 * ci.pair + t) * f.tpt + r / G;
+      if (r < f.tpt * G && tok < ci.n_new) look_again<T, D>(f, ci.seq, tok, ci.head * G + r % G, s_q[warp]);
+    }
+  }
+  if (!again) return;
+  // ---- marked sequences: a share of the rows that no block merged ----
+  const uint32_t warps = gridDim.x * gridDim.y * kWarps, me = (blockIdx.y * gridDim.x + blockIdx.x) * kWarps + warp;
+  for (int s = 0; s < f.a.seqs.n_seqs; ++s) {
+    if (!f.s.again[2 + s]) continue;
+    const int n_new = seq_at(f.a.cache, f.a.seqs, s).n_new;
+    for (int64_t i = me; i < (int64_t)n_new * f.a.cache.n_heads; i += warps) {
+      const int tok = (int)(i / f.a.cache.n_heads), g = (int)(i - (int64_t)tok * f.a.cache.n_heads);
+      bool merged = false;
+      for (uint32_t y = lane; y < gridDim.y; y += 32) {
+        const CutItem c = f.cuts[y];
+        merged |= c.parts != 0 && c.seq == s && c.head == g / G && c.pair == tok / (2 * f.tpt);
+      }
+      if (!__any_sync(0xffffffffu, merged)) look_again<T, D>(f, s, tok, g, s_q[warp]);
+    }
+  }
+  // the last block to come clears the marks
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    s_last = atomicAdd(f.s.again + 1, 1u) == gridDim.x * gridDim.y - 1;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  for (int s = threadIdx.x; s < f.a.seqs.n_seqs; s += blockDim.x) f.s.again[2 + s] = 0;
+  if (threadIdx.x == 0) f.s.again[0] = f.s.again[1] = 0;
 }
 
 }  // namespace

@@ -63,6 +63,29 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
                ::"r"(dst), "l"(map), "r"(c), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");
 }
 
+template <bool BF16>
+__device__ __forceinline__ float number(uint32_t u) {      // of 16 bits
+  return BF16 ? __uint_as_float(u << 16) : __half2float(__ushort_as_half((unsigned short)u));
+}
+// Whether some value of the first `tokens` of a step (at `v` in shared memory) is not finite; the same in the whole warp.  Adding the
+// exponent's lowest bit to an exponent of ones carries into the place of the sign.
+template <int D, bool BF16>
+__device__ __forceinline__ bool strange_values(uint32_t v, int tokens) {
+  constexpr uint32_t kExp = BF16 ? 0x7F807F80u : 0x7C007C00u, kOne = BF16 ? 0x00800080u : 0x04000400u;
+  const int lane = threadIdx.x & 31;
+  uint32_t strange = 0;
+#pragma unroll
+  for (int i = 0; i < Few<D>::kHalf / 512; ++i) {          // 4 rows of 128 bytes at a time, 16 rows a slab
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(v + 512 * i + 16 * lane) : "memory");
+    uint32_t x = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x |= (w[j] & kExp) + kOne;
+    if (4 * (i & 3) + (lane >> 3) < tokens) strange |= x;
+  }
+  return __any_sync(0xffffffffu, (strange & 0x80008000u) != 0);
+}
+
 // The parts of items in a block's piece, one after the other.
 struct FewWalk {
   uint32_t pos, end, cost;               // on the line, which has cost + units places per item
@@ -198,6 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
       }
     }
     const int least = a.full ? walk.len : walk.len - walk.n_new + 1;     // tokens below it are seen by every row
+    const bool several = least < walk.len;                               // some token is seen by some rows only
     float o[D / 8][4];
 #pragma unroll
     for (int j = 0; j < D / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
@@ -258,23 +282,45 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
       // ---- P V ----
       {
         const int row = (((lane >> 3) & 1) << 3) + (lane & 7);
-        const uint32_t at = base + C::kHalf + row * 128;
+        const uint32_t at0 = base + C::kHalf, at = at0 + row * 128;
         // tokens behind the end may hold anything, NaN included, which a weight of 0 would not silence: their rows count as zero
-        const bool tail = key + kStep > walk.len;
+        const bool tail = key + kStep > walk.len, hides = several && key + kStep > least;
         uint32_t mask0 = 0xffffffffu, mask1 = 0xffffffffu;
         if (tail) {
           const int k0 = key + 2 * t;
           mask0 = (k0 < walk.len ? 0xffffu : 0u) | (k0 + 1 < walk.len ? 0xffff0000u : 0u);
           mask1 = (k0 + 8 < walk.len ? 0xffffu : 0u) | (k0 + 9 < walk.len ? 0xffff0000u : 0u);
         }
+        if (hides && strange_values<D, BF16>(at0, walk.len - key)) {
+          // Values that are not finite, of which some rows do not see all: 0 times such a value is a NaN.  Token by token, then, with those
+          // rows alone that see it (and the same weights, sums in fp32 as there).
+          for (int k = 0; k < kStep && key + k < walk.len; ++k) {
+            const int src = (lane & ~3) | ((k & 7) >> 1);
+            float w[2];
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-          const int chunk = (2 * j & 7) + (lane >> 4);
-          uint32_t b[4];
-          ldsm4t(at + (j >> 2) * (kStep * 128) + ((chunk ^ (row & 7)) << 4), b);
-          if (tail) { b[0] &= mask0; b[1] &= mask1; b[2] &= mask0; b[3] &= mask1; }
-          mma16816<BF16>(o[2 * j], p, b[0], b[1]);
-          mma16816<BF16>(o[2 * j + 1], p, b[2], b[3]);
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t u = __shfl_sync(0xffffffffu, k < 8 ? p[e] : p[e + 2], src);
+              w[e] = number<BF16>((k & 1) ? u >> 16 : u & 0xffffu);
+            }
+#pragma unroll
+            for (int j = 0; j < D / 8; ++j) {
+              const uint32_t u = ld_shared_u32(at0 + (j >> 3) * (kStep * 128) + k * 128 + (((j & 7) ^ (k & 7)) << 4) + 4 * t);
+              const float v0 = number<BF16>(u & 0xffffu), v1 = number<BF16>(u >> 16);
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (key + k < limit[e]) { o[j][2 * e] = fmaf(w[e], v0, o[j][2 * e]); o[j][2 * e + 1] = fmaf(w[e], v1, o[j][2 * e + 1]); }
+            }
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) {
+            const int chunk = (2 * j & 7) + (lane >> 4);
+            uint32_t b[4];
+            ldsm4t(at + (j >> 2) * (kStep * 128) + ((chunk ^ (row & 7)) << 4), b);
+            if (tail) { b[0] &= mask0; b[1] &= mask1; b[2] &= mask0; b[3] &= mask1; }
+            mma16816<BF16>(o[2 * j], p, b[0], b[1]);
+            mma16816<BF16>(o[2 * j + 1], p, b[2], b[3]);
+          }
         }
       }
       __syncwarp();                       // every lane has read the stage

@@ -61,14 +61,15 @@ bool params_ok(const xkv_paged_params* p) {
   return p->slot_stride >= p->head_dim;
 }
 
-// Workspace: the status word, then the scratch of attention for one block per multiprocessor (arrival counts, running
+// Workspace: the status word, then the scratch of attention for one block per multiprocessor (arrival counts, marks of sequences, running
 // maxima and sums, accumulators: two partial results per block).
-struct Layout { size_t off_count, off_cuts, off_ml, off_o, total; };
+struct Layout { size_t off_count, off_again, off_cuts, off_ml, off_o, total; };
 Layout make_layout(const xkv_paged_params* p, int sms) {
   Layout l;
   size_t off = 256;
   auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
   l.off_count = take((size_t)sms * sizeof(unsigned int));
+  l.off_again = take((size_t)(2 + p->max_seqs) * sizeof(unsigned int));
   l.off_cuts = take((size_t)sms * attn_chunk_cut_bytes());
   l.off_ml = take((size_t)2 * sms * kChunkRows * sizeof(float2));
   l.off_o = take((size_t)2 * sms * kChunkRows * p->head_dim * sizeof(float));
@@ -208,6 +209,7 @@ int xkv_paged_create(const xkv_paged_params* params, void* k_pages, void* v_page
   v.page_shift = log2_of(params->page_tokens); v.n_pages = params->n_pages;
   v.status = reinterpret_cast<int*>(c->ws);
   c->scratch.count = reinterpret_cast<unsigned int*>(c->ws + layout.off_count);
+  c->scratch.again = reinterpret_cast<unsigned int*>(c->ws + layout.off_again);
   c->scratch.ml = reinterpret_cast<float2*>(c->ws + layout.off_ml);
   c->scratch.o = reinterpret_cast<float*>(c->ws + layout.off_o);
   c->cuts = c->ws + layout.off_cuts;

@@ -120,6 +120,7 @@ struct PagedScratch {
   float* o;              // [2 * blocks][rows][head_dim] accumulators
   float2* ml;            // [2 * blocks][rows] running maximum (log2 units) and sum
   unsigned int* count;   // [blocks] arrivals at the item that starts in a block and goes on in the next one (0 between calls)
+  unsigned int* again;   // [2 + max_seqs] the chunk kernel's: whether any, blocks done, sequences with rows to look at again (0 between calls)
 };
 constexpr int kFewRows = 16;       // rows of the kernel for few rows (a tile of a warp's matrix instruction)
 constexpr int kChunkRows = 256;    // rows of the kernel for chunks (two tiles of tcgen05.mma)

@@ -136,7 +136,7 @@ def test_evict_from_a_page_that_is_not_there(paged, page):
         assert torch.equal(w.get(w.weights, 0, keep, dst)[h], x[:, h][idx])
 
 
-# ---- attention: rows that see nothing-------------------------------------------------------------
+# ---- attention: rows that see nothing, values that a row does not see ----------------------------
 
 @pytest.mark.parametrize("m", [
     dict(news=[6], lens=[2], heads=2, kv_heads=2), dict(news=[3, 2], lens=[1, 40], heads=4, kv_heads=1, d=128, dtype="fp16"),
@@ -153,6 +153,72 @@ def test_rows_without_a_token_beside_values_that_are_not_finite(paged, m, impl):
     for b, (n, l) in enumerate(zip(w.news, w.lens_list)):
         rows = slice(w.starts[b], w.starts[b] + max(0, n - l))
         assert (out[:, rows] == 0).all() and torch.isneginf(lse[:, rows]).all()
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+UNSEEN = [
+    # few rows
+    dict(news=[4, 3], lens=[200, 37], heads=4, kv_heads=2), dict(news=[16], lens=[16], heads=2, kv_heads=2, d=128, dtype="fp16"),
+    dict(news=[2, 1, 5], lens=[1030, 300, 5], heads=6, kv_heads=2, d=128, page=64), dict(news=[8, 7], lens=[2000, 1999], heads=2, kv_heads=1, dtype="fp16"),
+    # chunks: all of them cut between blocks, some, and sequences that see less than their new tokens
+    dict(news=[300], lens=[700], heads=4, kv_heads=2), dict(news=[130, 40], lens=[2000, 40], heads=4, kv_heads=1, d=128, page=64, dtype="fp16"),
+    dict(news=[700, 1, 300], lens=[700, 500, 1500], heads=16, kv_heads=16, pad=3), dict(news=[257, 140], lens=[900, 140], heads=16, kv_heads=8, d=128),
+    dict(news=[150], lens=[100], heads=5, kv_heads=1, dtype="fp16"), dict(news=[20], lens=[9000], heads=64, kv_heads=1, page=256),
+]
+
+
+@pytest.mark.parametrize("m", UNSEEN, ids=str)
+@pytest.mark.parametrize("impl", [1, 0])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_values_behind_a_token_never_reach_it(paged, m, impl, bad):
+    """Some channels of a new token's value are not finite: those channels of it and of the tokens behind it are not finite,
+    and nothing else differs from the definition."""
+    w = World(paged, **m)
+    clean, lse0, before = w.attend(impl=impl)
+    w.check_attention(clean, lse0, False, *before)
+    b = 0
+    n, l = w.news[b], w.lens_list[b]
+    v = w.v[b].clone()
+    for token in sorted({max(0, n - l), n // 2, n - 1}):
+        channels = torch.arange(w.d, device="cuda") % 7 == 3
+        slot = l - n + token
+        w.v[b][0, slot, channels] = bad
+        w.v[b][w.K - 1, slot, 0] = bad
+        w.put(b, slot, slot + 1)
+        out, lse, _ = w.attend(impl=impl)
+        reached = torch.zeros_like(out, dtype=torch.bool)
+        group = w.H // w.K
+        reached[:group, w.starts[b] + token:w.starts[b] + n] = channels
+        reached[w.H - group:, w.starts[b] + token:w.starts[b] + n, 0] = True
+        assert not torch.isfinite(out[reached]).any(), token
+        w.v[b] = v.clone()
+        w.put(b, slot, slot + 1)
+        w.check_attention(torch.where(reached, clean, out), lse, False, *before, tag=f"token {token}")
+        rest = slice(w.starts[b] + n, None)                     # (the other sequences to the bit)
+        assert torch.equal(bits(out[:, rest]), bits(clean[:, rest])) and torch.equal(bits(lse), bits(lse0))
+    again, _, _ = w.attend(impl=impl)
+    assert torch.equal(bits(again), bits(clean))
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+@pytest.mark.parametrize("m", [dict(news=[5], lens=[50], heads=2, kv_heads=1), dict(news=[400], lens=[900], heads=8, kv_heads=4),
+                               dict(news=[200], lens=[3000], heads=4, kv_heads=4, d=128, dtype="fp16", page=64)], ids=str)
+def test_values_that_are_nan_throughout(paged, m):
+    """From a token on every value is NaN: the tokens before it keep their results, the others are NaN in every channel."""
+    w = World(paged, **m)
+    clean, lse0, before = w.attend()
+    n, l = w.news[0], w.lens_list[0]
+    for token in (0, n // 3, n - 1):
+        slots = slice(l - n + token, l)
+        v = w.v[0].clone()
+        w.v[0][:, slots] = math.nan
+        w.put(0, l - n, l)
+        out, lse, _ = w.attend()
+        assert out[:, token:].isnan().all() and torch.equal(bits(lse), bits(lse0))
+        w.v[0] = v
+        w.put(0, l - n, l)
+        out[:, token:] = clean[:, token:]
+        w.check_attention(out, lse, False, *before, tag=f"token {token}")
     assert w.cache.xkv_paged_poll_status() == 0
 
 
