@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
-from dataclasses import dataclass, field
+from dataclasses import dataclass, field, replace
 
 from .xkv import XKV_E_INVALID, XkvError, _i32, _i64, _sz, _vp, lib
 
@@ -184,6 +184,21 @@ def xkv_rotary(params: RotaryParams, positions, q, k=None, q_out=None, k_out=Non
     return q_out, k_out
 
 
+class _Fixed:
+    """Attributes of `_fixed` are set once: the library has pointers and numbers of them, which another value would not reach."""
+    _fixed = frozenset()
+
+    def __setattr__(self, name, value):
+        if name in self._fixed and name in self.__dict__:
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed: make another {type(self).__name__}")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        if name in self._fixed:
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed")
+        object.__delattr__(self, name)
+
+
 @dataclass
 class PagedParams:
     n_heads: int
@@ -195,17 +210,18 @@ class PagedParams:
     dtype: str = "bf16"
 
 
-class PagedBatch:
+class PagedBatch(_Fixed):
     """The sequences of a call (xkv_paged_batch): q_start [n_seqs + 1], lens [n_seqs] and table [n_seqs][width] are
-    int32 CUDA tensors, read when the kernels run; n_tokens = rows of the token tensors, no sequence has more
-    than max_new new tokens."""
+    int32 CUDA tensors, read when the kernels run (their contents may change, the tensors are these); n_tokens = rows of the
+    token tensors, no sequence has more than max_new new tokens."""
+    _fixed = frozenset(("device", "n_seqs", "n_tokens", "max_new", "q_start", "lens", "table", "struct", "ref"))
 
     def __init__(self, q_start, lens, table, n_tokens: int, max_new: int):
         where = "PagedBatch"
         _t()
         _require(lens.dim() == 1 and table.dim() == 2 and lens.is_cuda, where, "lens is [n_seqs], table [n_seqs][width], on a GPU")
         self.device, n = lens.get_device(), lens.shape[0]
-        self.n_seqs, self.n_tokens = n, n_tokens
+        self.n_seqs, self.n_tokens, self.max_new = n, n_tokens, max_new
         self.q_start, self.lens, self.table = q_start, lens, table
         self.struct = xkv_paged_batch(n, n_tokens, max_new, table.shape[1],
                                       _ints(q_start, where, "q_start", self.device, (n + 1,)),
@@ -214,15 +230,17 @@ class PagedBatch:
         self.ref = C.byref(self.struct)
 
 
-class PagedCache:
+class PagedCache(_Fixed):
     """A handle on two pools of pages, [n_pages][n_kv_heads][page_tokens][d] views of any order with contiguous
     channels, and on the weights of their slots (fp32 [n_pages][n_kv_heads][page_tokens], contiguous; optional).
-    The caller owns the pools; the handle owns its workspace."""
+    The caller owns the pools; the handle owns its workspace.  p is a copy: changing it changes nothing."""
+    _fixed = frozenset(("p", "device", "dtype", "k_pages", "v_pages", "weights", "workspace", "_heads", "_kv_heads", "_head_dim"))
 
     def __init__(self, p: PagedParams, k_pages, v_pages, weights=None):
         torch = _t()
         where = "xkv_paged_create"
-        self.p = p
+        self.p = p = replace(p)
+        self._heads, self._kv_heads, self._head_dim = p.n_heads, p.n_kv_heads, p.head_dim
         self.handle = _vp()
         _require(p.dtype in _DTYPE_NAMES, where, "dtype is bf16 or fp16")
         self.dtype = torch.bfloat16 if p.dtype == "bf16" else torch.float16
@@ -262,7 +280,7 @@ class PagedCache:
     def _shape(self, where: str, batch: PagedBatch, heads: int) -> tuple:
         if batch.device != self.device:
             _refuse(where, "the batch is on another device")
-        return heads, batch.n_tokens, self.p.head_dim
+        return heads, batch.n_tokens, self._head_dim
 
     # ---- the C calls, same names ------------------------------------------
     def kv_paged_append(self, batch: PagedBatch, k, v, q=None, q_out=None, rotary: RotaryParams | None = None, positions=None):
@@ -270,11 +288,11 @@ class PagedCache:
         a new tensor unless given.  Returns q_out."""
         where = "kv_paged_append"
         device, dtype = self.device, self.dtype
-        shape = self._shape(where, batch, self.p.n_kv_heads)
+        shape = self._shape(where, batch, self._kv_heads)
         rk, rv = _rows(k, where, "k", device, dtype, shape), _rows(v, where, "v", device, dtype, shape)
         rq = ro = _ABSENT
         if q is not None:
-            shape = (self.p.n_heads, batch.n_tokens, self.p.head_dim)
+            shape = (self._heads, batch.n_tokens, self._head_dim)
             if q_out is None:
                 q_out = _torch.empty_like(q)
             rq, ro = _rows(q, where, "q", device, dtype, shape), _rows(q_out, where, "q_out", device, dtype, shape)
@@ -292,7 +310,7 @@ class PagedCache:
         """Attention of the new tokens over what their sequences hold; out is a new tensor unless given, lse (fp32
         [n_heads][n_tokens], contiguous) is filled if given.  Returns out."""
         where = "attn_paged_causal"
-        shape = self._shape(where, batch, self.p.n_heads)
+        shape = self._shape(where, batch, self._heads)
         if out is None:
             out = _torch.zeros_like(q)        # rows that belong to nobody are not written
         rq, ro = _rows(q, where, "q", self.device, self.dtype, shape), _rows(out, where, "out", self.device, self.dtype, shape)
@@ -310,7 +328,7 @@ class PagedCache:
         """weights = decay * weights + what the new tokens' softmax gave every cached token (q, lse, scale and mask as
         in attn_paged_causal)."""
         where = "kv_paged_weights"
-        shape = self._shape(where, batch, self.p.n_heads)
+        shape = self._shape(where, batch, self._heads)
         rq = _rows(q, where, "q", self.device, self.dtype, shape)
         _call(self.device, lib.kv_paged_weights, where, self.handle, batch.ref, _pack1(*rq), self._lse(lse, where, shape),
               self.scale if scale is None else scale, decay, mask)
@@ -323,12 +341,12 @@ class PagedCache:
         if batch.device != device or dst_table.dim() != 2:
             _refuse(where, "dst_table is [n_seqs][width], the batch on the same device")
         if kept is None:
-            kept = _torch.empty(n, self.p.n_kv_heads, max(keep, 0), dtype=_int32, device=dst_table.device)
+            kept = _torch.empty(n, self._kv_heads, max(keep, 0), dtype=_int32, device=dst_table.device)
         if lens_out is None:
             lens_out = _torch.empty(n, dtype=_int32, device=dst_table.device)
         width = dst_table.shape[1]
         _call(device, lib.kv_paged_evict, where, self.handle, batch.ref, _ints(dst_table, where, "dst_table", device, (n, width)), width,
-              keep, n_first, n_recent, _ints(kept, where, "kept", device, (n, self.p.n_kv_heads, max(keep, 0))),
+              keep, n_first, n_recent, _ints(kept, where, "kept", device, (n, self._kv_heads, max(keep, 0))),
               _ints(lens_out, where, "lens_out", device, (n,)))
         return kept, lens_out
 

@@ -315,3 +315,19 @@ def test_append_beside_a_sequence_out_of_bounds(paged, start):
         assert w.cache.xkv_paged_poll_status() == -1
         w.news = [n if b in good else 0 for b, n in enumerate(news)]
         w.check_attention(out, lse, False, *before, tag=f"impl {impl}")
+
+
+# ---- batches and caches whose attributes somebody tries to change ------------------------------------
+
+def test_attributes_are_fixed(paged):
+    w = World(paged, news=[3], lens=[20])
+    out, lse, before = w.attend()
+    for x, name in ((w.batch, "lens"), (w.batch, "q_start"), (w.batch, "table"), (w.cache, "k_pages"), (w.cache, "workspace"), (w.cache, "weights")):
+        with pytest.raises(AttributeError, match=name):
+            setattr(x, name, torch.zeros_like(getattr(x, name)))
+    w.p.n_heads, w.cache.p.n_heads = 8, 2                      # (the handle's own numbers stay)
+    with pytest.raises(Exception):
+        w.cache.attn_paged_causal(w.batch, w.q[:2].contiguous())
+    again, _, _ = w.attend()
+    assert torch.equal(bits(again), bits(out))
+    w.check_attention(again, lse, False, *before)
