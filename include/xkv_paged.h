@@ -143,8 +143,10 @@ XKV_API int attn_paged_causal(xkv_paged* cache, const xkv_paged_batch* batch, co
  * over the new tokens and over the query heads of h: exp(q.k * softmax_scale - lse).  q and lse are those of attn_paged_causal
  * with the same mask.  Every slot of every sequence with new tokens is updated.  decay >= 0; with 0 the old
  * weights are not read.  A row with a NaN (in its query or its lse) makes every slot that it sees NaN; a row that saw nothing (lse
- * -infinity) gives nothing.  Sums are formed in a fixed order: the same call repeats exactly.
- * A slot that two sequences of the call share gets the update of one of them.  Errors: XKV_E_LIMIT as above. */
+ * -infinity) gives nothing.  Sums are formed in a fixed order: the same call repeats exactly, but for shared slots.
+ * Sequences of one call that share a page (a common prefix): with decay 1 its slots get the updates of all of them, added in
+ * any order; with another decay that of one of them, which one is not determined.  (A handle per sequence, on the same pages with
+ * weights of its own, keeps what each gave apart.)  Errors: XKV_E_LIMIT as above. */
 XKV_API int kv_paged_weights(xkv_paged* cache, const xkv_paged_batch* batch, const xkv_rows* q, const float* lse,
                      float softmax_scale, float decay, int32_t mask, xkv_stream stream);
 

@@ -171,6 +171,7 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
     const uint32_t buf = u + 2 * odd, scores = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 128 * buf;
     const uint64_t sc2 = pack_f2(a.scale_log2, a.scale_log2);
     uint32_t cnt = 0, ph = 0;                // tiles of the block so far; phase of this group's buffer
+    const bool adds = a.decay == 1.f, fades = a.decay != 0.f && !adds;
     uint32_t sum_at = 0, sum_ph = 0;         // place where the next item's parities meet, and its phase
     for (; walk.next(f, prefix, seqs); cnt += (uint32_t)walk.tiles) {
       const int token = walk.first + kUnit * (int)u + key;
@@ -230,7 +231,7 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
         if (in && !place) {
           if ((unsigned)page < (unsigned)a.cache.n_pages) {
             place = a.cache.weights + weight_offset(a.cache, page, walk.head, token);
-            if (a.decay != 0.f) old = *place;
+            if (fades) old = *place;
           } else {
             paged_report(a.cache.status, (int)XKV_E_INVALID);
           }
@@ -241,7 +242,10 @@ weights_kernel(const __grid_constant__ WeighArgs f, const __grid_constant__ Pool
             __syncwarp();
             total += s_sum[(2 * sum_at + u) * 128 + key];
           }
-          if (place) *place = a.decay * old + total;
+          if (place) {
+            // (added where nothing fades, so that sequences that share the slot lose no update)
+            if (adds) atomicAdd(place, total); else *place = a.decay * old + total;
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(b_lfree + 8 * at);

@@ -326,7 +326,7 @@ class PagedCache(_Fixed):
 
     def kv_paged_weights(self, batch: PagedBatch, q, lse, scale: float | None = None, decay: float = 1.0, mask: int = MASK_CAUSAL) -> None:
         """weights = decay * weights + what the new tokens' softmax gave every cached token (q, lse, scale and mask as
-        in attn_paged_causal)."""
+        in attn_paged_causal).  Slots that sequences of the batch share get all updates with decay 1, else one of them."""
         where = "kv_paged_weights"
         shape = self._shape(where, batch, self._heads)
         rq = _rows(q, where, "q", self.device, self.dtype, shape)

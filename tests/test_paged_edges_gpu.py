@@ -317,6 +317,53 @@ def test_append_beside_a_sequence_out_of_bounds(paged, start):
         w.check_attention(out, lse, False, *before, tag=f"impl {impl}")
 
 
+# ---- pages that several sequences read --------------------------------------------------------------
+
+def test_shared_pages(paged):
+    """Two sequences with a common prefix on the same pages: attention in one call; weights through a handle each, with weights
+    of their own, or through calls one after the other, which add up."""
+    P, prefix, d = 16, 160, 64
+    w = World(paged, news=[3, 2], lens=[prefix + 40, prefix + 25], page=P)
+    w.table[1, :prefix // P] = w.table[0, :prefix // P]
+    w.k[1][:, :prefix], w.v[1][:, :prefix] = w.k[0][:, :prefix], w.v[0][:, :prefix]
+    out, lse, before = w.attend()
+    w.check_attention(out, lse, False, *before)
+    sums = [w.weight_sums(b, False, lse) for b in range(2)]
+    one = [paged.PagedBatch(torch.tensor([w.starts[b], w.starts[b + 1]], dtype=torch.int32, device="cuda"), w.lens[b:b + 1].clone(),
+                            w.table[b:b + 1].clone(), w.rows, 3) for b in range(2)]
+    own = [torch.zeros_like(w.weights) for _ in range(2)]
+    for b in range(2):
+        paged.PagedCache(w.p, w.k_pages, w.v_pages, own[b]).kv_paged_weights(one[b], w.q, lse)
+        got, room = w.get(own[b], b, w.lens_list[b]).double(), sums[b][1]
+        assert ((got - sums[b][0]).abs() <= room + 2.0 ** -22 * sums[b][0]).all()
+    w.weights.zero_()
+    for b in range(2):
+        w.cache.kv_paged_weights(one[b], w.q, lse)
+    got = w.get(w.weights, 0, prefix).double()
+    want, room = sums[0][0][:, :prefix] + sums[1][0][:, :prefix], sums[0][1][:, :prefix] + sums[1][1][:, :prefix]
+    assert ((got - want).abs() <= room + 2.0 ** -22 * want).all()
+
+
+@pytest.mark.parametrize("m", [dict(heads=4, kv_heads=2, news=[1] * 12), dict(heads=2, kv_heads=2, d=128, dtype="fp16", news=[140, 200, 1, 30, 7])], ids=str)
+def test_weights_of_a_shared_prefix_add_up(paged, m):
+    """Sequences that share their first pages, in one call without fading: a slot gets what all of them gave it."""
+    prefix, B = 320, len(m["news"])
+    w = World(paged, lens=[prefix + n + 9 * b for b, n in enumerate(m["news"])], **m)
+    for b in range(1, B):
+        w.table[b, :prefix // w.P] = w.table[0, :prefix // w.P]
+        w.k[b][:, :prefix] = w.k[0][:, :prefix]
+    lse = lse_of(w, False)
+    sums = [w.weight_sums(b, False, lse) for b in range(B)]
+    before = w.weights.clone()
+    w.cache.kv_paged_weights(w.batch, w.q, lse)
+    shared = sum(s[:, :prefix] for s, _ in sums), sum(r[:, :prefix] for _, r in sums)
+    for b in range(B):
+        got, old = w.get(w.weights, b, w.lens_list[b]).double(), w.get(before, b, w.lens_list[b]).double()
+        want, room = (torch.cat([x, y[:, prefix:]], 1) for x, y in zip(shared, sums[b]))
+        assert ((got - old - want).abs() <= room + (B + 3) * 2.0 ** -24 * (want + old)).all(), b       # (B + 3 roundings of the running sum)
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
 # ---- batches and caches whose attributes somebody tries to change ------------------------------------
 
 def test_attributes_are_fixed(paged):
