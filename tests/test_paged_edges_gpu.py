@@ -364,6 +364,139 @@ def test_weights_of_a_shared_prefix_add_up(paged, m):
     assert w.cache.xkv_paged_poll_status() == 0
 
 
+# ---- enough work for the rings to go round ------------------------------------------------------------
+
+def multiprocessors():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def units_per_block(w, full, rows):
+    """Units of 128 tokens that a block has of the attention's line: an item is `rows` rows of a sequence and a key head."""
+    toks, units, items = rows // (w.H // w.K), 0, 0
+    for n, l in zip(w.news, w.lens_list):
+        for lo in range(0, n, toks):
+            seen = l if full else max(0, l - n + min(n, lo + toks))
+            units += w.K * max(1, -(-seen // 128))
+            items += w.K
+    return units / multiprocessors(), items / multiprocessors()
+
+
+CHUNKS = [dict(heads=16, kv_heads=16, page=64), dict(heads=16, kv_heads=16, d=128, dtype="fp16", page=128), dict(heads=32, kv_heads=8, d=128, page=32, order="slot"),
+          dict(heads=24, kv_heads=8, dtype="fp16", page=256)]
+
+
+def move(w, kind):
+    """Keys and queries whose scaled scores rise along the cache, fall, or jump, up to 50."""
+    scale = 50.0 / (w.d * w.scale)
+    for b, l in enumerate(w.lens_list):
+        x = torch.arange(l, device="cuda") / max(l, 1)
+        if kind == "falling":
+            x = 1 - x
+        elif kind == "steps":
+            x = ((x * 11).floor() % 4) / 4 + 0.25 * (torch.arange(l, device="cuda") % 97 == 50)
+        w.k[b] = (w.k[b].float() * 0.05 + (x * scale)[None, :, None]).to(w.dt)
+        w.put(b, 0, l)
+    sign = torch.where(torch.arange(w.n, device="cuda") % 3 == 1, -1.0, 1.0)[None, :, None]
+    head = torch.linspace(0.3, 1.0, w.H, device="cuda")[:, None, None]
+    w.q[:, :w.n] = (sign * head + 0.02 * w.q[:, :w.n].float()).to(w.dt)
+
+
+@pytest.mark.parametrize("m", CHUNKS, ids=str)
+@pytest.mark.parametrize("kind", ["random", "rising", "falling", "steps"])
+@pytest.mark.parametrize("full", [False, True])
+def test_chunks_of_many_units(paged, m, kind, full):
+    """Ten units of 128 tokens and more per block: the rings of K and V go round, and references move within a part."""
+    w = World(paged, news=[300, 150, 1, 40], lens=[6000, 4500, 2000, 1000], pad=5, **m)
+    units, items = units_per_block(w, full, 256)
+    assert units >= 10 and items >= 0.4
+    if kind != "random":
+        move(w, kind)
+    out, lse, before = w.attend(full)
+    w.check_attention(out, lse, full, *before)
+    again, _, _ = w.attend(full)
+    assert torch.equal(bits(again), bits(out))
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+@pytest.mark.parametrize("m", [dict(heads=16, kv_heads=16, page=64), dict(heads=16, kv_heads=8, d=128, dtype="fp16", page=16, order="slot")], ids=str)
+@pytest.mark.parametrize("full", [False, True])
+def test_chunks_of_many_items(paged, m, full):
+    """Parts of three items in most blocks: queries and accumulators are replaced."""
+    news = [257, 300, 513, 129, 260, 400, 130, 700]
+    w = World(paged, news=news, lens=[n + 300 * i for i, n in enumerate(news)], **m)
+    units, items = units_per_block(w, full, 256)
+    assert items >= 1.5 and units >= 10
+    out, lse, before = w.attend(full)
+    w.check_attention(out, lse, full, *before)
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+@pytest.mark.parametrize("m", [dict(heads=16, kv_heads=16, page=64), dict(heads=32, kv_heads=8, d=128, dtype="fp16", page=16, order="slot"),
+                               dict(heads=16, kv_heads=8, d=128, page=256)], ids=str)
+@pytest.mark.parametrize("kind", ["random", "rising", "falling", "steps"])
+@pytest.mark.parametrize("n", [1, 2])
+def test_few_rows_of_many_units(paged, m, kind, n):
+    """At least eight units per block, so that items have their cost in the cut, and rings of stages that go round."""
+    lens = [(1733 * i) % 6000 + n for i in range(30)] + [1, 9000]
+    w = World(paged, news=[n] * len(lens), lens=[max(l, n) for l in lens], pad=2, **m)
+    units, _ = units_per_block(w, False, 16)
+    assert units >= 10
+    if kind != "random":
+        move(w, kind)
+    out, lse, before = w.attend()
+    w.check_attention(out, lse, False, *before)
+    again, _, _ = w.attend()
+    assert torch.equal(bits(again), bits(out))
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+@pytest.mark.parametrize("m", [dict(heads=16, kv_heads=16, page=64, news=[200, 130, 300]), dict(heads=16, kv_heads=16, d=128, dtype="fp16", page=16, news=[129, 260, 140]),
+                               dict(heads=64, kv_heads=16, page=256, news=[70, 33, 100])], ids=str)
+@pytest.mark.parametrize("full", [False, True])
+def test_weights_of_many_items(paged, m, full):
+    """More than sixteen items per block, of two and more query tiles each, so that the places where their halves meet are used
+    again; and the same bits when the call is repeated."""
+    w = World(paged, lens=[17000, 15000, 12000], **m)
+    items = sum(-(-l // 256) for l in w.lens_list) * w.K / multiprocessors()
+    assert items >= 17 and all(n * w.H // w.K > 128 for n in w.news)
+    lse = lse_of(w, full)
+    before = w.weights.clone()
+    w.cache.kv_paged_weights(w.batch, w.q, lse, decay=0.5, mask=int(full))
+    first = w.weights.clone()
+    for b, l in enumerate(w.lens_list):
+        got, old = w.get(w.weights, b, l).double(), 0.5 * w.get(before, b, l).double()
+        want, room = w.weight_sums(b, full, lse)
+        assert ((got - want - old).abs() <= room + 2.0 ** -22 * (want + old)).all(), b
+    for _ in range(3):
+        w.weights.copy_(before)
+        w.cache.kv_paged_weights(w.batch, w.q, lse, decay=0.5, mask=int(full))
+        assert torch.equal(bits(w.weights), bits(first))
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+# ---- a missing page, in attention and weights ---------------------------------------------------------
+
+@pytest.mark.parametrize("m", [dict(news=[1, 1], lens=[200, 90]), dict(news=[3, 2], lens=[200, 90], d=128, dtype="fp16"),
+                               dict(news=[100, 20], lens=[400, 90], page=32), dict(news=[140, 20], lens=[700, 90], d=128, page=128)], ids=str)
+@pytest.mark.parametrize("full", [False, True])
+def test_a_page_that_is_not_there_reads_as_zero(paged, m, full):
+    w = World(paged, **m)
+    lo, hi = without_page(w, 0, 1)
+    for impl in (1, 0):
+        out, lse, before = w.attend(full, impl=impl)
+        assert w.cache.xkv_paged_poll_status() == -1
+        w.check_attention(out, lse, full, *before, tag=f"impl {impl}")
+    ref = lse_of(w, full)
+    w.weights.fill_(7.0)
+    w.cache.kv_paged_weights(w.batch, w.q, ref, decay=0.0, mask=int(full))
+    assert w.cache.xkv_paged_poll_status() == -1
+    slots = torch.cat([torch.arange(lo), torch.arange(hi, w.lens_list[0])]).cuda()
+    page, place = w.pages_of(slots, 0)
+    got = w.weights[page, :, place].T.double()
+    want, room = (x[:, slots] for x in w.weight_sums(0, full, ref))
+    assert ((got - want).abs() <= room + 2.0 ** -22 * want).all()
+
+
 # ---- batches and caches whose attributes somebody tries to change ------------------------------------
 
 def test_attributes_are_fixed(paged):
