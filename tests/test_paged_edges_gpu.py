@@ -511,3 +511,63 @@ def test_attributes_are_fixed(paged):
     again, _, _ = w.attend()
     assert torch.equal(bits(again), bits(out))
     w.check_attention(again, lse, False, *before)
+
+
+# ---- arguments that the other tests leave at their defaults ------------------------------------------
+
+FORMS = [dict(news=[1, 1], lens=[700, 33], heads=8, kv_heads=2), dict(news=[3, 2], lens=[300, 40], heads=4, kv_heads=1, d=128, dtype="fp16"),
+         dict(news=[150, 300], lens=[400, 900], heads=4, kv_heads=2), dict(news=[700, 40], lens=[1500, 40], heads=16, kv_heads=16, d=128, dtype="fp16", page=64),
+         dict(news=[1, 20], lens=[50, 90], heads=64, kv_heads=64), dict(news=[9], lens=[300], heads=63, kv_heads=1, d=128)]
+
+
+@pytest.mark.parametrize("m", FORMS, ids=str)
+@pytest.mark.parametrize("full", [False, True])
+def test_another_scale(paged, m, full):
+    w = World(paged, **m)
+    w.scale *= 2.5
+    for impl in (1, 0):
+        out = torch.full_like(w.q, 7.0)
+        lse = torch.full((w.H, w.rows), 7.0, device="cuda")
+        before = out.clone(), lse.clone()
+        w.cache.attn_paged_causal(w.batch, w.q, out=out, lse=lse, scale=w.scale, mask=int(full), impl=impl)
+        w.check_attention(out, lse, full, *before, tag=f"impl {impl}")
+    ref = lse_of(w, full)
+    w.cache.kv_paged_weights(w.batch, w.q, ref, scale=w.scale, decay=0.0, mask=int(full))
+    for b, l in enumerate(w.lens_list):
+        want, room = w.weight_sums(b, full, ref)
+        assert ((w.get(w.weights, b, l).double() - want).abs() <= room + 2.0 ** -22 * want).all(), b
+    assert w.cache.xkv_paged_poll_status() == 0
+
+
+@pytest.mark.parametrize("m", FORMS, ids=str)
+def test_output_in_place_of_the_queries(paged, m):
+    w = World(paged, **m)
+    for impl in (1, 0):
+        for full in (False, True):
+            out, lse, before = w.attend(full, impl)
+            w.check_attention(out, lse, full, *before)
+            x = w.q.clone()
+            w.cache.attn_paged_causal(w.batch, x, out=x, mask=int(full), impl=impl)
+            assert torch.equal(bits(x[:, :w.n]), bits(out[:, :w.n])) and torch.equal(bits(x[:, w.n:]), bits(w.q[:, w.n:]))
+
+
+def test_batch_smaller_than_the_handle(paged):
+    """A handle for 1024 sequences, calls of three of them, one after the other with other numbers."""
+    w = World(paged, news=[200, 1, 40], lens=[300, 90, 40], heads=4, kv_heads=2)
+    w.p.max_seqs = 1024
+    cache = paged.PagedCache(w.p, w.k_pages, w.v_pages, w.weights)
+    w.cache = cache
+    for _ in range(2):
+        out, lse, before = w.attend()
+        w.check_attention(out, lse, False, *before)
+        slot = w.lens_list[0] - 50
+        v = w.v[0][:, slot].clone()
+        w.v[0][:, slot] = math.nan
+        w.put(0, slot, slot + 1)
+        odd, _, _ = w.attend()
+        assert odd[:, 150:200].isnan().all()
+        w.v[0][:, slot] = v
+        w.put(0, slot, slot + 1)
+        odd[:, 150:200] = out[:, 150:200]
+        w.check_attention(odd, lse, False, *before)
+    assert cache.xkv_paged_poll_status() == 0
