@@ -137,15 +137,6 @@ struct ChunkWalk {
 __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr, uint32_t lbo) {        // make_desc with a leading byte offset
   return make_desc(saddr) - ((uint64_t)1 << 16) + ((uint64_t)(lbo >> 4) << 16);
 }
-__device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int c, int slot, int head, int page, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-               ::"r"(dst), "l"(map), "r"(c), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int c, int head, int tok, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-               ::"r"(dst), "l"(map), "r"(c), "r"(head), "r"(tok), "r"(bar) : "memory");
-}
-
 // Maxima of two pairs of 16-bit numbers, NaN where either is.
 template <bool BF16>
 __device__ __forceinline__ uint32_t max_nan_pair(uint32_t a, uint32_t b) {

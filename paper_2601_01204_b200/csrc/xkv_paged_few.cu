@@ -57,12 +57,6 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// One box of a pool: 64 channels from `c`, 16 slots from `slot` of (page, head).  A page that does not exist reads as zero.
-__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, int c, int slot, int head, int page, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-               ::"r"(dst), "l"(map), "r"(c), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");
-}
-
 template <bool BF16>
 __device__ __forceinline__ float number(uint32_t u) {      // of 16 bits
   return BF16 ? __uint_as_float(u << 16) : __half2float(__ushort_as_half((unsigned short)u));
@@ -191,9 +185,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const __grid_cons
       const int slot = a_key & ((1 << a.cache.page_shift) - 1);
       mbar_expect_tx(b, C::kStage);
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) tma_page(dst + c * kStep * 128, &maps.k, 64 * c, slot, ahead.head, page, b);
+      for (int c = 0; c < D / 64; ++c) tma_4d(dst + c * kStep * 128, &maps.k, 64 * c, slot, ahead.head, page, b);
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) tma_page(dst + C::kHalf + c * kStep * 128, &maps.v, 64 * c, slot, ahead.head, page, b);
+      for (int c = 0; c < D / 64; ++c) tma_4d(dst + C::kHalf + c * kStep * 128, &maps.v, 64 * c, slot, ahead.head, page, b);
     }
     ++put;
     a_key += kSpan;

@@ -2,6 +2,7 @@
 // descriptors, packed arithmetic.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <stdint.h>
@@ -258,6 +259,17 @@ __device__ __forceinline__ uint32_t make_idesc(int n_dim, bool bf16, bool b_mn_m
   d |= (uint32_t)(n_dim >> 3) << 17;
   d |= (uint32_t)(128 >> 4) << 24;
   return d;
+}
+
+// Copies by tensor map: a box of a pool (64 channels from `c`, slots from `slot` of a head and page; a page outside the map reads as zero) and
+// of a token tensor.
+__device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int c, int slot, int head, int page, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(dst), "l"(map), "r"(c), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int c, int head, int tok, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(c), "r"(head), "r"(tok), "r"(bar) : "memory");
 }
 
 __device__ __forceinline__ uint32_t swz_off(int row, int chunk) {
