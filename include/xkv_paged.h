@@ -47,6 +47,8 @@ typedef struct {
  *     original_tokens = 0:  all of them, w_i / factor;
  *     otherwise by bands: a pair that turns r = original_tokens * w_i / 2pi times over the trained length keeps
  *     w_i if r >= beta_fast, has w_i / factor if r <= beta_slow, and between them a blend that is linear in r.
+ *     (In r, not in the pair's index i: checkpoints whose frequencies blend linearly in i, between the pairs that turn beta_fast and
+ *     beta_slow times, have others in between, which this struct cannot state.)
  * Angles are formed in 64 bits (positions far beyond 2^24 keep theirs), sine, cosine and products in 32. */
 typedef struct {
   int32_t rotary_dim;        /* turned channels of one axis: even, n_axes * rotary_dim <= head_dim  */

@@ -19,8 +19,10 @@
 // that the next scores are computed during the softmax.  head_dim 128: the accumulators take half of the 512 columns and a
 // tile has 128 for its scores, whose first half P overwrites; the other tile's MMAs fill the time.
 //
-// Measured: a frame of 1374 queries over 16384 tokens, 16 heads of 64, 135 us (680 TFLOP/s; the exponentials alone need 80); chunks of
-// four prompts, 32 / 8 heads of 128, 525 us (1.01 PFLOP/s).  What bounds it is the chain scores -> exponentials -> P -> accumulator.
+// P is rounded to the type of V for its product, as in the kernel for few rows; sums, maxima, accumulators and parts are fp32.
+//
+// Measured: a frame of 1374 queries over 16384 tokens, 16 heads of 64, 137 us (673 TFLOP/s; the exponentials alone need 80); chunks of
+// four prompts, 32 / 8 heads of 128, 522 us (1.02 PFLOP/s, at 1.53 GHz and 980 W).  What bounds it is the chain scores -> exponentials -> P -> accumulator.
 //
 // Values that are not finite.  P is 0 where a row does not see a token, and 0 times a NaN or an infinity of V is a NaN: a new token's
 // value that is not finite would reach the tokens before it.  A softmax warp that writes a NaN behind a finite sum

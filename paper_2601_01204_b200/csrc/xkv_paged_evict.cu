@@ -6,7 +6,8 @@
 // the selection.  Ties go to the lower slot.
 //
 // Measured: eight sequences up to 16 385 tokens cut to 8192, 8 key heads of 128: 79 us, of which the rows take 52 (5.2 TB/s) and the
-// selection 22 (its latencies and a block's instructions per token); 1285 tokens of 16 heads cut to 1024: 9.7 us.
+// selection 22 (its latencies and a block's instructions per token; two of the eight sequences are longer than 8192, which is 16
+// blocks, and the copies wait for them); 1285 tokens of 16 heads cut to 1024: 9.7 us.
 #include "xkv_paged_internal.cuh"
 
 namespace xkv {

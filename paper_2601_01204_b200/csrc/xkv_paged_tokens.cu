@@ -6,8 +6,8 @@
 // that they turn (40 heads of 128 channels) 1.3 MB of traffic.  After that a thread moves 16 or 32 bytes of a row
 // at a time: a pair of 16-byte pieces half an axis apart, or one piece of interleaved pairs.
 //
-// What bounds it is memory: 8192 tokens of 32 + 8 heads of 128 channels 32 us (5.2 TB/s), 4043 tokens of four prompts into their pages
-// 23.6 us (4.2 TB/s); one token per sequence is a launch (4.4 us in a graph).
+// What bounds it is memory: 8192 tokens of 32 + 8 heads of 128 channels 33 us (5.1 TB/s), 4043 tokens of four prompts into their pages
+// 23 us (4.3 TB/s); one token per sequence is a launch (4.4 us in a graph).
 #include "xkv_paged_internal.cuh"
 
 namespace xkv {

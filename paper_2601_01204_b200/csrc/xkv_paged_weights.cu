@@ -17,7 +17,7 @@
 // What bounds it: with many rows the exponentials (16 per clock and multiprocessor; a quarter of them are polynomials on the FMA
 // pipes; the MMAs need a quarter to a half of that time), with few rows reading K.  Measured: a frame of 1374 queries over 16384
 // tokens, 16 heads of 64, 96 us (107 without the polynomials; the exponentials alone 80 on the special-function unit); 16 single
-// tokens over 38 880, 8 key heads of 128, 23.6 us.
+// tokens over 38 880, 8 key heads of 128, 22.8 us.
 #include "xkv_paged_line.cuh"
 #include "xkv_ptx.cuh"
 

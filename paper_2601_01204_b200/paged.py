@@ -3,6 +3,8 @@ argument marshalling only.
 
 Every step runs in the library's CUDA kernels, on torch's current stream of the tensors' device.  torch is
 used for device memory and streams.  There is no CPU fallback.
+No call takes part in autograd: results carry no gradient, whatever the inputs ask for (xkv_rotary with inverse=True takes
+gradients of its outputs to gradients of its inputs).
 """
 from __future__ import annotations
 
